@@ -1,138 +1,22 @@
 // Host runtime of the HeadCast routed-attention library: context, validation,
 // per-layer head tables and compact buffers (Sec. 4.3), work lists of the
 // head-specific attention (Sec. 4.4), and the one-time online classification
-// (Sec. 4.2, Eq. 2-5).  Every entry point of include/headcast.h lives here.
+// (Sec. 4.2, Eq. 2-5).  The entry points of the operators beside them are in hc_ops.cpp.
 #include "headcast.h"
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <memory>
-#include <new>
-#include <string>
 #include <vector>
 
-#include "hc_internal.h"
-#include "hc_plan.h"
+#include "hc_context.h"
 
 using namespace hc;
 
 namespace {
-
-struct DevBuf {
-  void *p = nullptr;
-  size_t bytes = 0;
-};
-
-struct Layer {
-  bool has_types = false;
-  std::vector<uint8_t> types;
-  std::vector<int32_t> slot;
-  std::vector<int> sd_heads, sp_heads, g_heads;
-  int64_t cur_block = -1;
-  // the compact buffers: parts of one allocation, `kv`
-  DevBuf kv, k_sd, v_sd, k_g, v_g, k_sp, v_sp;
-  // dense work units and, behind them, combine items of the current plan
-  DevBuf plan;
-  const DenseUnit *units = nullptr;
-  const CombineItem *comb = nullptr;
-  int n_units = 0, n_comb = 0;
-  bool plan_wide = false;      // 128-dim heads: the units run on waves of 64 queries
-  int64_t plan_slots = 0;      // partial slots that the units write
-  int plan_nv = -1;            // valid window blocks the plan was built for
-  bool plan_used = false;      // launches may still read the plan's memory
-  hipStream_t kv_stream = nullptr;   // the stream that last wrote the compact buffers
-  int static_nv = -1;          // window fill that `chosen` is for
-  StaticChoice chosen{};       // the device-built work list
-  int sp_split = 1;            // key-frame split of the Spatial work (full window)
-};
-
-struct EventPair {
-  hipEvent_t a, b;
-};
-
-}  // namespace
-
-struct hc_ctx {
-  hc_config cfg{};
-  int device = 0;
-  float scale = 0.f;
-  int L = 0, P = 0;
-  SpatialGeom geo{};          // frame storage of the Spatial buffers (centred window)
-  int64_t sd_keys = 0, g_keys = 0, sp_keys = 0;
-  std::vector<Layer> layers;
-  std::string err;
-  bool profile = false;
-  std::vector<EventPair> pending[HC_K_COUNT];
-  std::vector<EventPair> pool;
-  double prof_ms[HC_K_COUNT] = {};
-  int64_t prof_n[HC_K_COUNT] = {};
-  DevBuf part;                 // partial-result slots shared by all layers
-  int64_t part_slots = 0;
-  DevBuf sp_part, sp_ml;       // Spatial split partials shared by all layers
-  int64_t sp_part_rows = 0;
-  int n_cu = 0;                // compute units of the device
-  // cell variant of the Spatial path (cfg.spatial_cell > 0)
-  CellTables cells;
-  DevBuf cell_off_d, qmap_d;   // cells.off and cells.qmap on the device
-  // device memory of hc_classify_heads, allocated (and zeroed) by the first call
-  // and reused by the next ones: the window in Global and in Spatial layout, the
-  // four proxy outputs, the block partials, the work lists, the token statistics
-  DevBuf cls_k, cls_v, cls_pk, cls_pv, cls_o[4], cls_part, cls_units, cls_comb, cls_tok;
-  int cls_n_units = 0, cls_n_comb = 0;
-  bool cls_wide = false;       // 128-dim heads: the sweep runs on waves of 64 queries
-  bool cls_done = false;       // cls_o holds the outputs of a successful classification
-  void *scratch = nullptr;     // this device's fixed scratch (hc_attention_static)
-  // the last choices of hc_attention_static: layers with as many heads of each kind
-  // at the same window fill share one
-  struct {
-    int n_g, n_sd, nv;
-    bool merged;
-    StaticChoice choice;
-  } static_memo[16];
-  int static_memos = 0;        // choices made
-};
-
-namespace {
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-hc_status fail(hc_ctx *c, hc_status s, const char *fmt, ...) {
-  if (c) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    try {
-      c->err = buf;
-    } catch (const std::bad_alloc &) {
-      c->err.clear();
-    }
-  }
-  return s;
-}
-
-// Ends the functions that allocate host memory: nothing is thrown across the ABI.
-#define HC_NO_HOST_MEMORY(ctx) \
-  catch (const std::bad_alloc &) { return fail(ctx, HC_E_NOMEM, "out of host memory"); }
-
-// A failed HIP call stays the thread's last error until it is read, and the next
-// launch would take it for its own: every failure that is reported or passed over
-// here is read off first.
-#define HC_HIP(ctx, call)                                                               \
-  do {                                                                                  \
-    hipError_t e_ = (call);                                                             \
-    if (e_ != hipSuccess) {                                                             \
-      (void)hipGetLastError();                                                          \
-      return fail(ctx, e_ == hipErrorOutOfMemory ? HC_E_NOMEM : HC_E_DEVICE, "%s: %s", \
-                  #call, hipGetErrorString(e_));                                        \
-    }                                                                                   \
-  } while (0)
 
 hc_status dev_malloc(hc_ctx *c, DevBuf &b, size_t bytes) {
   const hipError_t e = hipMalloc(&b.p, bytes);
@@ -175,43 +59,6 @@ void free_layer(Layer &l) {
   l.k_sd = l.v_sd = l.k_g = l.v_g = l.k_sp = l.v_sp = DevBuf{};
   drop_plan(l);
   l.plan_used = false;
-}
-
-// --- profiling ----------------------------------------------------------------
-hc_status prof_begin(hc_ctx *c, hipStream_t s, EventPair *ep) {
-  if (!c->profile) return HC_OK;
-  if (c->pool.empty()) {
-    EventPair p;
-    HC_HIP(c, hipEventCreate(&p.a));
-    const hipError_t e = hipEventCreate(&p.b);
-    if (e != hipSuccess) {
-      (void)hipEventDestroy(p.a);
-      (void)hipGetLastError();
-      return fail(c, HC_E_DEVICE, "hipEventCreate: %s", hipGetErrorString(e));
-    }
-    c->pool.push_back(p);
-  }
-  *ep = c->pool.back();
-  c->pool.pop_back();
-  HC_HIP(c, hipEventRecord(ep->a, s));
-  return HC_OK;
-}
-
-hc_status prof_end(hc_ctx *c, hipStream_t s, int kind, const EventPair &ep) {
-  if (!c->profile) return HC_OK;
-  HC_HIP(c, hipEventRecord(ep.b, s));
-  c->pending[kind].push_back(ep);
-  return HC_OK;
-}
-
-template <class F>
-hc_status timed_launch(hc_ctx *c, hipStream_t s, int kind, F &&launch) {
-  EventPair ep{};
-  hc_status st = prof_begin(c, s, &ep);
-  if (st != HC_OK) return st;
-  hipError_t e = launch();
-  if (e != hipSuccess) return fail(c, HC_E_DEVICE, "kernel launch: %s", hipGetErrorString(e));
-  return prof_end(c, s, kind, ep);
 }
 
 // --- geometry helpers ---------------------------------------------------------------
