@@ -272,14 +272,171 @@ hc_status hc_attention_static(hc_ctx *ctx, int layer, const void *q, const uint8
  * slots, and the classification memory once hc_classify_heads has run). */
 hc_status hc_memory_bytes(const hc_ctx *ctx, int64_t *bytes);
 
+/* ---------------------------------------------------------------------------
+ * Operators beside the routed attention: what a model runs before it (rotary
+ * positions), the attention over whole prompts and clips, and a cache held in 4
+ * bits with its attention.  They take a context for its device, its message
+ * (hc_last_error) and its kernel timing only: sizes and heads are arguments of
+ * the call, not the context's.  They allocate nothing, copy nothing and do not
+ * synchronise, so they may be captured into a HIP graph; a call that needs room for
+ * partial results takes it from the caller, and two graphs (or two calls at once)
+ * need a workspace each.  The calling thread's current device is left as it was.
+ * Pointers are 16-byte aligned unless said otherwise, strides are in elements and
+ * multiples of 8 (neighbouring dims of a head are always 1 apart).  Lengths and
+ * offsets in device memory are read when the call runs: they cannot be checked
+ * by the host, and values out of range are clamped, so that nothing outside the
+ * given tensors is read or written.
+ * ------------------------------------------------------------------------- */
+enum { HC_BF16 = 0, HC_F32 = 1 };
+
+/* Rotary positions over several axes.  The first rot = sum(axis_dims) dims of
+ * every head form rot / 2 pairs: dims (2i, 2i + 1), or (i, i + rot / 2) with
+ * `halves`.  axis_dims[0] / 2 pairs turn with the position on axis 0, the next
+ * axis_dims[1] / 2 with that on axis 1, and so on, by the angle
+ * position * theta^(-2 j / m): j counts the pairs of the axis and m = axis_dims, or
+ * with `joint` j counts all pairs and m = rot.  (a, b) becomes
+ * (a cos - b sin, a sin + b cos); with `inverse` the angle's sign changes, which
+ * also is the gradient of the rotation.  Dims behind rot are copied.  Angles are
+ * computed in 64 bits, the rotation in 32, and rounded once to the output's type.
+ *
+ * Positions: int32 [n_axes][n_tokens] in device memory (4-byte aligned), or NULL for the
+ * tokens of consecutive frames (n_axes = 3: frame, row, column): token t is at frame
+ * frame0 + t / (grid_h grid_w), row t / grid_w % grid_h, column t % grid_w. */
+typedef struct {
+  const void *x;             /* [n_tokens][n_heads][head_dim] by the strides below       */
+  void *out;                 /* may be x itself with equal strides and types, and may
+                              * not overlap it otherwise                                 */
+  int64_t x_token, x_head, out_token, out_head;
+  int32_t n_heads;           /* >= 1                                                     */
+} hc_rotate_tensor;
+
+typedef struct {
+  int32_t n_tokens;          /* 0 does nothing                                           */
+  int32_t head_dim;          /* a multiple of 8, at most 256                             */
+  int32_t x_type, out_type;  /* HC_BF16 or HC_F32, for all tensors of the call           */
+  int32_t n_axes;            /* 1..4                                                     */
+  int32_t axis_dims[4];      /* even; their sum is a multiple of 16, at most head_dim     */
+  int32_t halves, joint, inverse;
+  int32_t grid_h, grid_w, frame0;
+  double theta;              /* > 0, finite                                              */
+  const int32_t *positions;
+} hc_rotate_args;
+
+/* Rotates one or two tensors (a block's queries and keys) of the same tokens in one
+ * launch.  Async. */
+hc_status hc_rotate(hc_ctx *ctx, const hc_rotate_args *args, const hc_rotate_tensor *tensors,
+                    int n_tensors, hc_stream stream);
+
+/* Attention over packed sequences: prompts, clips, or blocks over their own text.
+ * The queries of sequence s are rows cu_q[s] .. cu_q[s+1] - 1 of q, its keys rows
+ * cu_k[s] .. cu_k[s+1] - 1 of k and v (bfloat16).  Query head h reads key head
+ * h / (n_heads / n_kv_heads).  With n queries and m keys, query i of a sequence sits at
+ * position p = m - n + i and sees, of the m keys,
+ *   causal_block = 0      all,
+ *   causal_block = c > 0  those before (p / c + 1) c, none if p < 0: c = 1 is the
+ *                         causal mask, c = block_tokens lets a block see itself and
+ *                         every earlier block.
+ * A query that sees nothing gets zeros.  Output rows outside every sequence are
+ * left as they were.  A NaN or infinity in a sequence's own keys or values may reach
+ * any of that sequence's queries, and no other sequence's. */
+typedef struct {
+  const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
+  void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; overlaps no input     */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  int32_t n_tokens;          /* rows of q and out; 0 does nothing                        */
+  int32_t n_keys;            /* rows of k and v                                          */
+  int32_t n_seqs;            /* >= 1                                                     */
+  int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads                      */
+  int32_t head_dim;          /* 64 or 128                                                */
+  int32_t causal_block;      /* >= 0                                                     */
+  float softmax_scale;       /* 0 => 1/sqrt(head_dim)                                    */
+  const int32_t *cu_q;       /* device [n_seqs + 1] (4-byte aligned); NULL: n_seqs equal
+                              * parts (n_tokens a multiple of n_seqs)                    */
+  const int32_t *cu_k;       /* NULL: the queries' offsets (n_keys = n_tokens then)       */
+  void *workspace;           /* hc_packed_workspace bytes, NULL if that is 0              */
+  int64_t workspace_bytes;
+} hc_packed_args;
+
+/* Bytes of workspace that hc_packed_attention needs for these arguments (its device
+ * pointers are not read).  Pure host. */
+hc_status hc_packed_workspace(hc_ctx *ctx, const hc_packed_args *args, int64_t *bytes);
+hc_status hc_packed_attention(hc_ctx *ctx, const hc_packed_args *args, hc_stream stream);
+
+/* A cache of keys and values in 4 bits, in memory of the caller: n_seqs sequences of
+ * up to `capacity` tokens, hc_qcache_bytes bytes at `data`.  Every 32 neighbouring dims
+ * of a token share a power of two 2^e, and each is stored as the nearest of
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6 times 2^e with its sign (ties to an even code).  For the
+ * largest magnitude a of the 32, 2^k <= a < 2^(k+1): e = k - 2, or k - 1 if a > 7/4 2^k,
+ * so that no value is off by more than half a step; e stays in [-125, 125].  If one
+ * of the 32 is infinite or NaN, all of them read back as NaN.  The layout inside is the
+ * library's own.  Slots that were never written hold nothing that is read, as long as
+ * lengths say so: memory need not be cleared. */
+typedef struct {
+  void *data;
+  int32_t n_seqs;            /* >= 1                                                     */
+  int32_t n_heads;           /* key heads, >= 1                                          */
+  int32_t head_dim;          /* 64 or 128                                                */
+  int32_t capacity;          /* tokens per sequence, >= 1                                */
+} hc_qcache;
+
+hc_status hc_qcache_bytes(const hc_qcache *cache, int64_t *bytes);   /* `data` is not read */
+
+/* Tokens for (append) or from (read) the cache: rows cu_seqlens[s] .. cu_seqlens[s+1] - 1
+ * of k and v are slots start[s], start[s] + 1, ... of sequence s (NULL cu_seqlens: n_seqs
+ * equal parts).  Rows whose slot lies outside [0, capacity), or that belong to no sequence,
+ * are neither stored nor written.  A slot may be written again (a block's next denoising
+ * step, a ring of blocks).  Async. */
+typedef struct {
+  void *k, *v;               /* bf16 [n_tokens][n_heads][head_dim] by the strides below; hc_qcache_append
+                              * only reads them                                          */
+  int64_t k_token, k_head, v_token, v_head;
+  int32_t n_tokens;          /* 0 does nothing                                           */
+  const int32_t *start;      /* device [n_seqs] (4-byte aligned)                          */
+  const int32_t *cu_seqlens; /* device [n_seqs + 1], or NULL                              */
+} hc_qcache_rows;
+
+hc_status hc_qcache_append(hc_ctx *ctx, const hc_qcache *cache, const hc_qcache_rows *rows,
+                           hc_stream stream);
+hc_status hc_qcache_read(hc_ctx *ctx, const hc_qcache *cache, const hc_qcache_rows *rows,
+                         hc_stream stream);
+
+/* Attention of new queries over the first kv_len[s] slots of each sequence, with the
+ * position and mask rules of hc_packed_attention (m = kv_len[s]).  The keys and values
+ * are the stored 4-bit ones; q and the probabilities are bfloat16, sums float32.
+ * With a ring of blocks (slots not in the order of positions) use causal_block = 0.
+ * kv_len is clamped to [0, capacity]. */
+typedef struct {
+  const void *q;             /* bf16 [n_tokens][n_heads][head_dim]                        */
+  void *out;                 /* bf16, the same shape; does not overlap q                  */
+  int64_t q_token, q_head, out_token, out_head;
+  int32_t n_tokens;          /* 0 does nothing                                           */
+  int32_t n_heads;           /* a multiple of the cache's heads                           */
+  int32_t causal_block;
+  int32_t max_kv;            /* about the longest kv_len, 0 if unknown: the key range of a
+                              * query is split by it; the result does not depend on it
+                              * beyond rounding                                          */
+  float softmax_scale;       /* 0 => 1/sqrt(head_dim)                                    */
+  const int32_t *kv_len;     /* device [n_seqs] (4-byte aligned)                          */
+  const int32_t *cu_seqlens; /* device [n_seqs + 1]; NULL: n_seqs equal parts             */
+  void *workspace;           /* hc_qcache_workspace bytes, NULL if that is 0              */
+  int64_t workspace_bytes;
+} hc_qcache_attention_args;
+
+hc_status hc_qcache_workspace(hc_ctx *ctx, const hc_qcache *cache,
+                              const hc_qcache_attention_args *args, int64_t *bytes);
+hc_status hc_qcache_attention(hc_ctx *ctx, const hc_qcache *cache,
+                              const hc_qcache_attention_args *args, hc_stream stream);
+
 /* Kernel timing: when enabled, every launch the context makes records a pair
  * of HIP events on the stream it is launched on.  hc_profile_read synchronises
  * those events and returns the summed duration (ms) and the launch count of
  * one kernel kind since the last reset, then resets it.  A merge of partials
  * counts as HC_K_COMBINE; one of Spatial ranges alone is timed with its
- * HC_K_SPATIAL launch. */
+ * HC_K_SPATIAL launch.  HC_K_SEQUENCE is hc_packed_attention and
+ * hc_qcache_attention (the merge of their key ranges included), HC_K_CACHE hc_qcache_append and
+ * hc_qcache_read. */
 enum { HC_K_DENSE = 0, HC_K_SPATIAL = 1, HC_K_SCATTER = 2, HC_K_STATS = 3, HC_K_COMBINE = 4,
-       HC_K_COUNT = 5 };
+       HC_K_ROTATE = 5, HC_K_SEQUENCE = 6, HC_K_CACHE = 7, HC_K_COUNT = 8 };
 hc_status hc_profile_enable(hc_ctx *ctx, int on);
 hc_status hc_profile_read(hc_ctx *ctx, int kernel_kind, double *total_ms, int64_t *launches);
 

@@ -12,7 +12,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libheadcast.so")
-SOURCES = ["hc_runtime.cpp", "hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip"]
+SOURCES = ["hc_runtime.cpp", "hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip",
+           "hc_ops.cpp", "hc_rotate.hip", "hc_qcache.hip", "hc_seq.hip", "hc_decode.hip"]
 
 
 def hipcc() -> str:

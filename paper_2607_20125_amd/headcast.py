@@ -17,14 +17,17 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libheadcast
 HC_OK, HC_E_INVAL, HC_E_STATE, HC_E_ORDER, HC_E_NOMEM, HC_E_DEVICE = 0, -1, -2, -3, -4, -5
 SINK, DUMMY, SPATIAL, GLOBAL = 0, 1, 2, 3
 N_STATS = 6
-K_DENSE, K_SPATIAL, K_SCATTER, K_STATS, K_COMBINE = 0, 1, 2, 3, 4
+K_DENSE, K_SPATIAL, K_SCATTER, K_STATS, K_COMBINE, K_ROTATE, K_SEQUENCE, K_CACHE = range(8)
+BF16, F32 = 0, 1
 CLS_O_REF, CLS_O_SINK, CLS_O_DUMMY, CLS_O_SPATIAL = 0, 1, 2, 3
 
 EXPORTS = ("hc_config_default", "hc_validate_config", "hc_status_string", "hc_last_error",
            "hc_ring_slot", "hc_create", "hc_destroy", "hc_classify_heads", "hc_classify_outputs",
            "hc_set_head_types",
            "hc_get_layout", "hc_append_block", "hc_attention", "hc_attention_static",
-           "hc_memory_bytes", "hc_profile_enable", "hc_profile_read")
+           "hc_memory_bytes", "hc_profile_enable", "hc_profile_read",
+           "hc_rotate", "hc_packed_workspace", "hc_packed_attention", "hc_qcache_bytes",
+           "hc_qcache_append", "hc_qcache_read", "hc_qcache_workspace", "hc_qcache_attention")
 STATIC_SCRATCH_BYTES = 64 << 20   # HC_STATIC_SCRATCH_BYTES
 
 
@@ -35,6 +38,48 @@ class HCConfig(ctypes.Structure):
         (n, ctypes.c_float) for n in (
             "theta_sink", "theta_dummy", "theta_spatial", "theta_score", "gamma",
             "softmax_scale")] + [("spatial_cell", ctypes.c_int32), ("sd_blocks", ctypes.c_int32)]
+
+
+def _fields(*groups):
+    """ctypes fields from (type, "names") pairs."""
+    return [(n, kind) for kind, names in groups for n in names.split()]
+
+
+_P, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class HCRotateTensor(ctypes.Structure):
+    _fields_ = _fields((_P, "x out"), (_I64, "x_token x_head out_token out_head"), (_I32, "n_heads"))
+
+
+class HCRotateArgs(ctypes.Structure):
+    _fields_ = (_fields((_I32, "n_tokens head_dim x_type out_type n_axes"), (_I32 * 4, "axis_dims"),
+                        (_I32, "halves joint inverse grid_h grid_w frame0"),
+                        (ctypes.c_double, "theta"), (_P, "positions")))
+
+
+class HCPackedArgs(ctypes.Structure):
+    _fields_ = _fields((_P, "q k v out"),
+                       (_I64, "q_token q_head k_token k_head v_token v_head out_token out_head"),
+                       (_I32, "n_tokens n_keys n_seqs n_heads n_kv_heads head_dim causal_block"),
+                       (ctypes.c_float, "softmax_scale"), (_P, "cu_q cu_k workspace"),
+                       (_I64, "workspace_bytes"))
+
+
+class HCQCache(ctypes.Structure):
+    _fields_ = _fields((_P, "data"), (_I32, "n_seqs n_heads head_dim capacity"))
+
+
+class HCQCacheRows(ctypes.Structure):
+    _fields_ = _fields((_P, "k v"), (_I64, "k_token k_head v_token v_head"), (_I32, "n_tokens"),
+                       (_P, "start cu_seqlens"))
+
+
+class HCQCacheAttentionArgs(ctypes.Structure):
+    _fields_ = _fields((_P, "q out"), (_I64, "q_token q_head out_token out_head"),
+                       (_I32, "n_tokens n_heads causal_block max_kv"),
+                       (ctypes.c_float, "softmax_scale"), (_P, "kv_len cu_seqlens workspace"),
+                       (_I64, "workspace_bytes"))
 
 
 class HeadCastError(RuntimeError):
@@ -71,6 +116,21 @@ def _load() -> ctypes.CDLL:
         "hc_profile_enable": (ctypes.c_int, [P, ctypes.c_int]),
         "hc_profile_read": (ctypes.c_int, [P, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                                            ctypes.POINTER(I64)]),
+        "hc_rotate": (ctypes.c_int, [P, ctypes.POINTER(HCRotateArgs),
+                                     ctypes.POINTER(HCRotateTensor), ctypes.c_int, P]),
+        "hc_packed_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs),
+                                               ctypes.POINTER(I64)]),
+        "hc_packed_attention": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs), P]),
+        "hc_qcache_bytes": (ctypes.c_int, [ctypes.POINTER(HCQCache), ctypes.POINTER(I64)]),
+        "hc_qcache_append": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
+                                            ctypes.POINTER(HCQCacheRows), P]),
+        "hc_qcache_read": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
+                                          ctypes.POINTER(HCQCacheRows), P]),
+        "hc_qcache_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
+                                               ctypes.POINTER(HCQCacheAttentionArgs),
+                                               ctypes.POINTER(I64)]),
+        "hc_qcache_attention": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
+                                               ctypes.POINTER(HCQCacheAttentionArgs), P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -124,11 +184,32 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+class QCache:
+    """A cache of 4-bit keys and values (hc_qcache) in one uint8 tensor: `n_seqs`
+    sequences of up to `capacity` tokens.  `Context.qcache` makes one."""
+
+    def __init__(self, n_seqs: int, n_heads: int, head_dim: int, capacity: int, device):
+        import torch
+        for name, value in (("n_seqs", n_seqs), ("n_heads", n_heads), ("capacity", capacity)):
+            if not 1 <= value < 1 << 31:
+                raise ValueError(f"{name} must be at least 1 and below 2^31, got {value}")
+        self.desc = HCQCache(None, n_seqs, n_heads, head_dim, capacity)
+        nbytes = ctypes.c_int64()
+        st = lib.hc_qcache_bytes(ctypes.byref(self.desc), ctypes.byref(nbytes))
+        if st != HC_OK:
+            raise HeadCastError(st, f"hc_qcache_bytes: {status_string(st)}")
+        self.data = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
+        self.desc.data = self.data.data_ptr()
+        self.n_seqs, self.n_heads = n_seqs, n_heads
+        self.head_dim, self.capacity = head_dim, capacity
+
+
 class Context:
     """Owns one hc_ctx (all layers' compact buffers) on one device."""
 
     def __init__(self, cfg: HCConfig, device: int = 0):
         self.cfg = cfg
+        self.device = device
         self._h = ctypes.c_void_p()
         st = lib.hc_create(ctypes.byref(cfg), device, ctypes.byref(self._h))
         if st != HC_OK:
@@ -242,3 +323,157 @@ class Context:
         self._check(lib.hc_profile_read(self._h, kind, ctypes.byref(ms), ctypes.byref(n)),
                     "hc_profile_read")
         return ms.value, n.value
+
+    # --- operators beside the routed attention -----------------------------------
+    # Tensors are [tokens][heads][head_dim] with any token and head strides that are
+    # multiples of 8; a head-major tensor [heads][tokens][head_dim] is passed as
+    # t.transpose(0, 1).
+
+    def _current_stream(self):
+        import torch
+        return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _rows(self, name, t, dtypes, shape=None):
+        """Pointer and strides of a [tokens][heads][head_dim] tensor on this context's device."""
+        if t.dtype not in dtypes or not t.is_cuda or t.device.index != self.device:
+            raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))} on cuda:{self.device}, "
+                             f"got {t.dtype} on {t.device}")
+        if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[tokens][heads][head_dim]'}, "
+                             f"got {tuple(t.shape)}")
+        if t.numel() and t.shape[2] > 1 and t.stride(2) != 1:
+            raise ValueError(f"{name}: neighbouring dims of a head must be adjacent in memory")
+        # (the stride of an axis of length 1 says nothing and may be anything)
+        token = t.stride(0) if t.shape[0] > 1 else 0
+        head = t.stride(1) if t.shape[1] > 1 else 0
+        return ctypes.c_void_p(t.data_ptr()), token, head
+
+    def _ints(self, name, t, shape):
+        import torch
+        if t is None:
+            return None
+        if (t.dtype != torch.int32 or not t.is_cuda or t.device.index != self.device
+                or not t.is_contiguous() or tuple(t.shape) != tuple(shape)):
+            raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on "
+                             f"cuda:{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return ctypes.c_void_p(t.data_ptr())
+
+    def _work(self, args, nbytes, workspace):
+        """Puts a workspace of `nbytes` bytes into args: the caller's, or one that lives until
+        the tensor returned here is dropped (torch keeps its memory from other streams' work)."""
+        import torch
+        if nbytes == 0:
+            return None
+        if workspace is None:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{self.device}")
+        elif not workspace.is_cuda or workspace.device.index != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on cuda:{self.device}")
+        args.workspace = workspace.data_ptr()
+        args.workspace_bytes = workspace.numel() * workspace.element_size()
+        return workspace
+
+    def rotate(self, x, out=None, *, axis_dims, positions=None, grid=None, frame0=0,
+               theta=10000.0, halves=False, joint=False, inverse=False):
+        """hc_rotate: rotary positions over `len(axis_dims)` axes of one tensor or of a pair
+        (queries and keys of the same tokens).  `out`: a tensor or pair of the same shapes
+        (bf16 or float32; `x` itself rotates in place), new ones by default.  Positions:
+        int32 [axes][tokens], or the (frame, row, column) of the tokens of a `grid` of (height,
+        width), the context's by default, from frame `frame0` on.  Returns `out`."""
+        import torch
+        pair = isinstance(x, (tuple, list))
+        xs = list(x) if pair else [x]
+        if out is None:
+            outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
+        else:
+            outs = list(out) if isinstance(out, (tuple, list)) else [out]
+        if len(outs) != len(xs) or not 1 <= len(xs) <= 2:
+            raise ValueError("rotate takes one tensor or a pair, and as many outputs")
+        if not 1 <= len(axis_dims) <= 4:
+            raise ValueError("axis_dims must have one to four entries")
+        types = {torch.bfloat16: BF16, torch.float32: F32}
+        n, d = xs[0].shape[0], xs[0].shape[-1]
+        tensors = (HCRotateTensor * len(xs))()
+        for i, (t, o) in enumerate(zip(xs, outs)):
+            if t.dtype != xs[0].dtype or o.dtype != outs[0].dtype:
+                raise ValueError("both tensors of a pair must have the same type")
+            xp, xt, xh = self._rows("x", t, types, None if i == 0 else (n, t.shape[1], d))
+            op, ot, oh = self._rows("out", o, types, t.shape)
+            tensors[i] = HCRotateTensor(xp, op, xt, xh, ot, oh, t.shape[1])
+        gh, gw = grid if grid is not None else (self.cfg.grid_h, self.cfg.grid_w)
+        a = HCRotateArgs(n, d, types[xs[0].dtype], types[outs[0].dtype], len(axis_dims),
+                         (_I32 * 4)(*axis_dims), bool(halves), bool(joint), bool(inverse), gh, gw, frame0,
+                         theta, self._ints("positions", positions, (len(axis_dims), n)))
+        self._check(lib.hc_rotate(self._h, ctypes.byref(a), tensors, len(xs), self._current_stream()),
+                    "hc_rotate")
+        return tuple(outs) if pair else outs[0]
+
+    def packed_attention(self, q, k, v, cu_q=None, cu_k=None, out=None, *, causal_block=0,
+                         softmax_scale=0.0, workspace=None, n_seqs=None):
+        """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
+        cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
+        None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
+        import torch
+        bf16 = (torch.bfloat16,)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if n_seqs is None:
+            n_seqs = cu_q.shape[0] - 1 if cu_q is not None else 1
+        qp, qt, qh = self._rows("q", q, bf16)
+        kp, kt, kh = self._rows("k", k, bf16, (k.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None)
+        vp, vt, vh = self._rows("v", v, bf16, k.shape)
+        op, ot, oh = self._rows("out", out, bf16, q.shape)
+        a = HCPackedArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, q.shape[0], k.shape[0], n_seqs,
+                         q.shape[1], k.shape[1], q.shape[2], causal_block, softmax_scale,
+                         self._ints("cu_q", cu_q, (n_seqs + 1,)), self._ints("cu_k", cu_k, (n_seqs + 1,)))
+        need = ctypes.c_int64()
+        self._check(lib.hc_packed_workspace(self._h, ctypes.byref(a), ctypes.byref(need)),
+                    "hc_packed_workspace")
+        held = self._work(a, need.value, workspace)
+        self._check(lib.hc_packed_attention(self._h, ctypes.byref(a), self._current_stream()),
+                    "hc_packed_attention")
+        del held
+        return out
+
+    def qcache(self, n_seqs: int, n_heads: int, head_dim: int, capacity: int) -> QCache:
+        """A new 4-bit cache on this context's device."""
+        return QCache(n_seqs, n_heads, head_dim, capacity, f"cuda:{self.device}")
+
+    def _cache_rows(self, fn, what, cache, k, v, start, cu_seqlens):
+        import torch
+        shape = (k.shape[0], cache.n_heads, cache.head_dim)
+        kp, kt, kh = self._rows("k", k, (torch.bfloat16,), shape)
+        vp, vt, vh = self._rows("v", v, (torch.bfloat16,), shape)
+        r = HCQCacheRows(kp, vp, kt, kh, vt, vh, shape[0], self._ints("start", start, (cache.n_seqs,)),
+                         self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
+        self._check(fn(self._h, ctypes.byref(cache.desc), ctypes.byref(r), self._current_stream()), what)
+
+    def qcache_append(self, cache: QCache, k, v, start, cu_seqlens=None):
+        """hc_qcache_append: stores the rows of k and v (bf16 [tokens][cache heads][head_dim])
+        in slots start[s] .. of each sequence (int32 [n_seqs])."""
+        self._cache_rows(lib.hc_qcache_append, "hc_qcache_append", cache, k, v, start, cu_seqlens)
+
+    def qcache_read(self, cache: QCache, k, v, start, cu_seqlens=None):
+        """hc_qcache_read: writes the stored values of those slots into k and v."""
+        self._cache_rows(lib.hc_qcache_read, "hc_qcache_read", cache, k, v, start, cu_seqlens)
+
+    def qcache_attention(self, cache: QCache, q, kv_len, cu_seqlens=None, out=None, *,
+                         causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
+        """hc_qcache_attention: attention of q over the first kv_len[s] (int32 [n_seqs]) slots
+        of each sequence of the cache.  Returns `out` (bf16, the shape of q)."""
+        import torch
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qp, qt, qh = self._rows("q", q, (torch.bfloat16,),
+                                (q.shape[0], q.shape[1], cache.head_dim) if q.dim() == 3 else None)
+        op, ot, oh = self._rows("out", out, (torch.bfloat16,), q.shape)
+        a = HCQCacheAttentionArgs(qp, op, qt, qh, ot, oh, q.shape[0], q.shape[1], causal_block, max_kv,
+                                  softmax_scale, self._ints("kv_len", kv_len, (cache.n_seqs,)),
+                                  self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
+        need = ctypes.c_int64()
+        self._check(lib.hc_qcache_workspace(self._h, ctypes.byref(cache.desc), ctypes.byref(a),
+                                            ctypes.byref(need)), "hc_qcache_workspace")
+        held = self._work(a, need.value, workspace)
+        self._check(lib.hc_qcache_attention(self._h, ctypes.byref(cache.desc), ctypes.byref(a),
+                                            self._current_stream()), "hc_qcache_attention")
+        del held
+        return out
