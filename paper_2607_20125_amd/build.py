@@ -13,7 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libheadcast.so")
 SOURCES = ["hc_runtime.cpp", "hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip",
-           "hc_ops.cpp", "hc_rotate.hip", "hc_qcache.hip", "hc_seq.hip", "hc_decode.hip"]
+           "hc_ops.cpp", "hc_rotate.hip", "hc_qcache.hip", "hc_seq.hip", "hc_seq128.hip", "hc_decode.hip"]
 
 
 def hipcc() -> str:
@@ -50,7 +50,7 @@ def build_library(verbose: bool = False) -> str:
 
     with tempfile.TemporaryDirectory(prefix="headcast_build_") as tdir:
         objs = [os.path.join(tdir, src + ".o") for src in SOURCES]
-        cmds = [[hipcc()] + flags + ([] if src == "hc_dense128.hip" else vgpr_form)
+        cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip") else vgpr_form)
                 + ["-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
         with concurrent.futures.ThreadPoolExecutor(max_workers=len(cmds)) as ex:
             list(ex.map(run, cmds))

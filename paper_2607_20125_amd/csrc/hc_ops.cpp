@@ -87,10 +87,10 @@ int64_t unit_room(int64_t n_tokens, int64_t n_seqs, int64_t group, int R, bool a
 // Key ranges per unit.  A launch of fewer work groups than the card runs at once leaves
 // CUs idle, so key tiles are shared out until about `want` groups run, but no range is
 // shorter than `least` tiles: a partial result costs a write, a read and a merge launch.
-int choose_split(int64_t units, int64_t keys, int64_t want, int64_t least) {
+int choose_split(int64_t units, int64_t keys, int64_t want, int64_t least, int64_t most) {
   const int64_t tiles = (keys + kSeqKeys - 1) / kSeqKeys;
   const int64_t cuts = std::min(want / std::max<int64_t>(units, 1), tiles / least);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(cuts, 256));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(cuts, most));
 }
 
 hc_status run_seq(hc_ctx *c, const SeqArgs &a, int head_dim, bool few_rows, hipStream_t s) {
@@ -144,7 +144,9 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
   if (rows > INT32_MAX - kSeqRows || !good_grid(tiles * a.kv_heads))
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
-  a.n_split = choose_split(tiles * a.kv_heads, p->n_keys / p->n_seqs, 512, 8);
+  a.n_split = choose_split(tiles * a.kv_heads, p->n_keys / p->n_seqs, 512, 8, kSeqMaxSplit);
+  // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
+  a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24;
   if (!good_grid(tiles * a.kv_heads * a.n_split)) a.n_split = 1;
   return HC_OK;
 }
@@ -224,7 +226,9 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
   const int64_t keys = p->max_kv > 0 ? std::min(p->max_kv, k->capacity) : k->capacity;
-  a.n_split = choose_split(tiles * a.kv_heads, keys, few_rows ? 1024 : 512, few_rows ? 4 : 8);
+  a.n_split = choose_split(tiles * a.kv_heads, keys, few_rows ? 1024 : 512, few_rows ? 4 : 8,
+                           few_rows ? kDecodeMaxSplit : kSeqMaxSplit);
+  a.wide = k->head_dim == 128;
   if (!good_grid(tiles * a.kv_heads * a.n_split)) a.n_split = 1;
   return HC_OK;
 }

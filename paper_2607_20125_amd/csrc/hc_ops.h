@@ -1,5 +1,5 @@
 // Internal structures of the operators beside the routed attention (hc_ops.cpp,
-// hc_rotate.hip, hc_qcache.hip, hc_seq.hip, hc_decode.hip).  Not part of the public ABI.
+// hc_rotate.hip, hc_qcache.hip, hc_seq.hip, hc_seq128.hip, hc_decode.hip).  Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -61,6 +61,7 @@ hipError_t launch_qcache_read(const QCacheArgs &a, hipStream_t s);
 // (kDecodeRows in the kernel for few rows), and each unit's key tiles may be cut into
 // n_split ranges whose partial results a second launch merges.
 constexpr int kSeqRows = 128, kDecodeRows = 16, kSeqKeys = 64;
+constexpr int kSeqMaxSplit = 32, kDecodeMaxSplit = 256;
 struct SeqArgs {
   const uint16_t *q;
   uint16_t *o;
@@ -78,10 +79,12 @@ struct SeqArgs {
   int32_t n_split;
   float *part;                   // [kv_heads * tiles][n_split][rows (d + 2)]
   float scale_log2;              // softmax scale * log2(e)
+  bool wide;                     // 128-dim heads: waves of 64 rows (hc_seq128.hip)
 };
 // Floats of one partial result: rows of d sums, then the rows' maxima and sums.
 constexpr int64_t seq_part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
 hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_seq128(const SeqArgs &a, hipStream_t s);
 hipError_t launch_decode(const SeqArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_seq_merge(const SeqArgs &a, int head_dim, int rows, hipStream_t s);
 

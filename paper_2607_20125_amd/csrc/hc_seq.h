@@ -92,6 +92,9 @@ __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u)
     u.k0 = u.q0;
     u.nk = u.nq;
   }
+  // (loads from memory that the kernel might write: uniform all the same)
+  u.k0 = __builtin_amdgcn_readfirstlane((int)u.k0);
+  u.nk = __builtin_amdgcn_readfirstlane(u.nk);
   return true;
 }
 

@@ -303,10 +303,61 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = w;
 }
 
+// The same for many partial results: a work group takes one row, its threads 4 dims of every
+// 256 * 4 / D-th of them, so that their reads are in flight together.  (One thread summing all 128
+// of a long cache's row took 66 us beside an attention kernel of 29.)
+template <int D, int R>
+__global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
+  constexpr int TR = D / 4, NG = 256 / TR;
+  __shared__ float sW[kDecodeMaxSplit], sL[kDecodeMaxSplit], sO[NG][D], sM[4];
+  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
+  const int tile = rest / R, lrow = rest % R;
+  SeqUnit u;
+  if (!seq_unit<R>(a, tile, u)) return;
+  const int row = u.row0 + lrow;
+  if (row >= u.rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float *pp = a.part + ((int64_t)tile * a.kv_heads + head) * a.n_split * seq_part_floats(R, D);
+  const float *ml = pp + tid * seq_part_floats(R, D) + R * D + lrow;
+  const float m = tid < a.n_split ? ml[0] : kMInit;
+  const float l = tid < a.n_split ? ml[R] : 0.f;
+  float M = m;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) M = fmaxf(M, __shfl_xor(M, d));
+  if (lane == 0) sM[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sM[0], sM[1]), fmaxf(sM[2], sM[3]));
+  const float w = __builtin_amdgcn_exp2f(m - M);
+  sW[tid] = w;
+  sL[tid] = w * l;
+  __syncthreads();
+  const int grp = tid / TR, dim = tid % TR * 4;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const float *op = pp + lrow * D + dim;
+#pragma unroll 4
+  for (int i = grp; i < a.n_split; i += NG)
+    o += sW[i] * *reinterpret_cast<const f32x4 *>(op + i * seq_part_floats(R, D));
+  *reinterpret_cast<f32x4 *>(&sO[grp][dim]) = o;
+  __syncthreads();
+  if (tid >= TR) return;
+  float total = 0.f;
+  for (int i = 0; i < a.n_split; ++i) total += sL[i];
+#pragma unroll
+  for (int k = 1; k < NG; ++k) o += *reinterpret_cast<const f32x4 *>(&sO[k][dim]);
+  const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+  const int qi = row / a.group, qh = head * a.group + (row - qi * a.group);
+  const bf16x2 x = {(__bf16)(o[0] * inv), (__bf16)(o[1] * inv)}, y = {(__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
+  uint2 r;
+  r.x = __builtin_bit_cast(uint32_t, x);
+  r.y = __builtin_bit_cast(uint32_t, y);
+  *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = r;
+}
+
 }  // namespace
 
 hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
   const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * a.n_split)), block(64 * kWaves);
+  if (head_dim == 128 && a.wide) return launch_seq128(a, s);
   if (head_dim == 128) {
     if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<128, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((seq_attn_kernel<128, false>), grid, block, 0, s, a);
@@ -318,15 +369,20 @@ hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
 }
 
 hipError_t launch_seq_merge(const SeqArgs &a, int head_dim, int rows, hipStream_t s) {
-  const int per = rows * head_dim / 1024;      // work groups of a unit
+  const bool many = a.n_split > 8;
+  const int per = many ? rows : rows * head_dim / 1024;      // work groups of a unit
   const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * per)), block(256);
+#define HC_MERGE(D, R)                                                                     \
+  if (many) hipLaunchKernelGGL((seq_merge_many_kernel<D, R>), grid, block, 0, s, a);       \
+  else hipLaunchKernelGGL((seq_merge_kernel<D, R>), grid, block, 0, s, a)
   if (head_dim == 128) {
-    if (rows == kSeqRows) hipLaunchKernelGGL((seq_merge_kernel<128, kSeqRows>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((seq_merge_kernel<128, kDecodeRows>), grid, block, 0, s, a);
+    if (rows == kSeqRows) { HC_MERGE(128, kSeqRows); }
+    else { HC_MERGE(128, kDecodeRows); }
   } else {
-    if (rows == kSeqRows) hipLaunchKernelGGL((seq_merge_kernel<64, kSeqRows>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((seq_merge_kernel<64, kDecodeRows>), grid, block, 0, s, a);
+    if (rows == kSeqRows) { HC_MERGE(64, kSeqRows); }
+    else { HC_MERGE(64, kDecodeRows); }
   }
+#undef HC_MERGE
   return hipGetLastError();
 }
 

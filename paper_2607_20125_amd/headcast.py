@@ -8,6 +8,7 @@ raises on import instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -184,6 +185,19 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+@functools.lru_cache(maxsize=None)
+def _torch():
+    import torch
+    return torch
+
+
+def _raw_stream(device):
+    """torch's current stream of a device as a hipStream_t (the short way where torch has it)."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 class QCache:
     """A cache of 4-bit keys and values (hc_qcache) in one uint8 tensor: `n_seqs`
     sequences of up to `capacity` tokens.  `Context.qcache` makes one."""
@@ -210,6 +224,7 @@ class Context:
     def __init__(self, cfg: HCConfig, device: int = 0):
         self.cfg = cfg
         self.device = device
+        self._torch_device = f"cuda:{device}"
         self._h = ctypes.c_void_p()
         st = lib.hc_create(ctypes.byref(cfg), device, ctypes.byref(self._h))
         if st != HC_OK:
@@ -329,43 +344,36 @@ class Context:
     # multiples of 8; a head-major tensor [heads][tokens][head_dim] is passed as
     # t.transpose(0, 1).
 
-    def _current_stream(self):
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
-
     def _rows(self, name, t, dtypes, shape=None):
         """Pointer and strides of a [tokens][heads][head_dim] tensor on this context's device."""
-        if t.dtype not in dtypes or not t.is_cuda or t.device.index != self.device:
+        s, st = t.shape, t.stride()
+        if t.dtype not in dtypes or t.get_device() != self.device:
             raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))} on cuda:{self.device}, "
                              f"got {t.dtype} on {t.device}")
-        if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        if len(s) != 3 or (shape is not None and s != shape):
             raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[tokens][heads][head_dim]'}, "
-                             f"got {tuple(t.shape)}")
-        if t.numel() and t.shape[2] > 1 and t.stride(2) != 1:
+                             f"got {tuple(s)}")
+        if st[2] != 1 and s[2] > 1 and s[0] and s[1]:
             raise ValueError(f"{name}: neighbouring dims of a head must be adjacent in memory")
         # (the stride of an axis of length 1 says nothing and may be anything)
-        token = t.stride(0) if t.shape[0] > 1 else 0
-        head = t.stride(1) if t.shape[1] > 1 else 0
-        return ctypes.c_void_p(t.data_ptr()), token, head
+        return t.data_ptr(), st[0] if s[0] > 1 else 0, st[1] if s[1] > 1 else 0
 
     def _ints(self, name, t, shape):
-        import torch
         if t is None:
             return None
-        if (t.dtype != torch.int32 or not t.is_cuda or t.device.index != self.device
-                or not t.is_contiguous() or tuple(t.shape) != tuple(shape)):
+        if t.dtype is not _torch().int32 or t.get_device() != self.device or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on "
                              f"cuda:{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return ctypes.c_void_p(t.data_ptr())
+        return t.data_ptr()
 
     def _work(self, args, nbytes, workspace):
         """Puts a workspace of `nbytes` bytes into args: the caller's, or one that lives until
         the tensor returned here is dropped (torch keeps its memory from other streams' work)."""
-        import torch
         if nbytes == 0:
             return None
         if workspace is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{self.device}")
+            torch = _torch()
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self._torch_device)
         elif not workspace.is_cuda or workspace.device.index != self.device or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected a contiguous tensor on cuda:{self.device}")
         args.workspace = workspace.data_ptr()
@@ -379,7 +387,7 @@ class Context:
         (bf16 or float32; `x` itself rotates in place), new ones by default.  Positions:
         int32 [axes][tokens], or the (frame, row, column) of the tokens of a `grid` of (height,
         width), the context's by default, from frame `frame0` on.  Returns `out`."""
-        import torch
+        torch = _torch()
         pair = isinstance(x, (tuple, list))
         xs = list(x) if pair else [x]
         if out is None:
@@ -403,7 +411,7 @@ class Context:
         a = HCRotateArgs(n, d, types[xs[0].dtype], types[outs[0].dtype], len(axis_dims),
                          (_I32 * 4)(*axis_dims), bool(halves), bool(joint), bool(inverse), gh, gw, frame0,
                          theta, self._ints("positions", positions, (len(axis_dims), n)))
-        self._check(lib.hc_rotate(self._h, ctypes.byref(a), tensors, len(xs), self._current_stream()),
+        self._check(lib.hc_rotate(self._h, ctypes.byref(a), tensors, len(xs), _raw_stream(self.device)),
                     "hc_rotate")
         return tuple(outs) if pair else outs[0]
 
@@ -412,7 +420,7 @@ class Context:
         """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
         cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
         None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
-        import torch
+        torch = _torch()
         bf16 = (torch.bfloat16,)
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -429,7 +437,7 @@ class Context:
         self._check(lib.hc_packed_workspace(self._h, ctypes.byref(a), ctypes.byref(need)),
                     "hc_packed_workspace")
         held = self._work(a, need.value, workspace)
-        self._check(lib.hc_packed_attention(self._h, ctypes.byref(a), self._current_stream()),
+        self._check(lib.hc_packed_attention(self._h, ctypes.byref(a), _raw_stream(self.device)),
                     "hc_packed_attention")
         del held
         return out
@@ -439,13 +447,13 @@ class Context:
         return QCache(n_seqs, n_heads, head_dim, capacity, f"cuda:{self.device}")
 
     def _cache_rows(self, fn, what, cache, k, v, start, cu_seqlens):
-        import torch
+        torch = _torch()
         shape = (k.shape[0], cache.n_heads, cache.head_dim)
         kp, kt, kh = self._rows("k", k, (torch.bfloat16,), shape)
         vp, vt, vh = self._rows("v", v, (torch.bfloat16,), shape)
         r = HCQCacheRows(kp, vp, kt, kh, vt, vh, shape[0], self._ints("start", start, (cache.n_seqs,)),
                          self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
-        self._check(fn(self._h, ctypes.byref(cache.desc), ctypes.byref(r), self._current_stream()), what)
+        self._check(fn(self._h, ctypes.byref(cache.desc), ctypes.byref(r), _raw_stream(self.device)), what)
 
     def qcache_append(self, cache: QCache, k, v, start, cu_seqlens=None):
         """hc_qcache_append: stores the rows of k and v (bf16 [tokens][cache heads][head_dim])
@@ -460,7 +468,7 @@ class Context:
                          causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
         """hc_qcache_attention: attention of q over the first kv_len[s] (int32 [n_seqs]) slots
         of each sequence of the cache.  Returns `out` (bf16, the shape of q)."""
-        import torch
+        torch = _torch()
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         qp, qt, qh = self._rows("q", q, (torch.bfloat16,),
@@ -474,6 +482,6 @@ class Context:
                                             ctypes.byref(need)), "hc_qcache_workspace")
         held = self._work(a, need.value, workspace)
         self._check(lib.hc_qcache_attention(self._h, ctypes.byref(cache.desc), ctypes.byref(a),
-                                            self._current_stream()), "hc_qcache_attention")
+                                            _raw_stream(self.device)), "hc_qcache_attention")
         del held
         return out
