@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int split = rest % a.n_split, tile = rest / a.n_split;
   SeqUnit u;
-  if (!seq_unit<R>(a, tile, u)) return;
+  if (!seq_unit<R>(a, tile, u)) return no_unit(a, tile, head, split);
 
   const int at = min(u.row0 + i, u.rows - 1);
   const int qi = at / a.group, qh = head * a.group + (at - qi * a.group);
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
   const int last = min(u.row0 + R, u.rows) - 1;
   const int lo_all = seen_keys(a, u, u.row0 / a.group), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
-  const int t0 = (int)((int64_t)nt_all * split / a.n_split);
-  const int t1 = (int)((int64_t)nt_all * (split + 1) / a.n_split);
+  int t0, t1;
+  key_range(a, u, tile, head, split, nt_all, t0, t1);
   const float sl2 = a.scale_log2;
   const uint8_t *base = a.cache + ((int64_t)u.seq * a.kv_heads + head) * a.cache_head;
 

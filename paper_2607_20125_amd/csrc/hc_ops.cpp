@@ -84,13 +84,21 @@ int64_t unit_room(int64_t n_tokens, int64_t n_seqs, int64_t group, int R, bool a
   return n_tokens * group / R + std::min(n_seqs, n_tokens);
 }
 
-// Key ranges per unit.  A launch of fewer work groups than the card runs at once leaves
-// CUs idle, so key tiles are shared out until about `want` groups run, but no range is
+// Key ranges per unit.  A launch of fewer work groups than the card runs at once leaves CUs
+// idle, so key tiles are shared out until about `want` groups run, but no range is
 // shorter than `least` tiles: a partial result costs a write, a read and a merge launch.
-int choose_split(int64_t units, int64_t keys, int64_t want, int64_t least, int64_t most) {
-  const int64_t tiles = (keys + kSeqKeys - 1) / kSeqKeys;
-  const int64_t cuts = std::min(want / std::max<int64_t>(units, 1), tiles / least);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(cuts, most));
+void choose_split(SeqArgs &a, int64_t keys, int64_t want, int64_t least, int64_t most) {
+  const int64_t units = (int64_t)a.tiles * a.kv_heads, tiles = (keys + kSeqKeys - 1) / kSeqKeys;
+  const int64_t cuts = std::min({want / std::max<int64_t>(units, 1), tiles / least, most});
+  a.n_split = cuts < 2 || !good_grid(units * cuts) ? 1 : (int32_t)cuts;
+}
+
+// 128-dim heads: waves of 64 rows, which run the matrix cores better but start slowly and hide
+// nothing of it (one wave per SIMD), or of 32.  9360 rows of 12 heads (900 work groups) over 256, 512 and
+// 1024 keys: 37, 50 and 75 us against 33, 55 and 95; 1024 rows (96 groups, a
+// part of the card) over 512, 1024 and 2048 keys: 20, 27 and 34 us against 18, 25 and 36.
+bool wide_rows(const SeqArgs &a, int64_t keys) {
+  return keys >= ((int64_t)a.tiles * a.kv_heads * a.n_split >= 256 ? 384 : 1536);
 }
 
 hc_status run_seq(hc_ctx *c, const SeqArgs &a, int head_dim, bool few_rows, hipStream_t s) {
@@ -110,7 +118,13 @@ hc_status check_workspace(hc_ctx *c, const void *p, int64_t bytes, int64_t neede
 }
 
 int64_t part_bytes(const SeqArgs &a, int head_dim, int rows) {
-  return a.n_split == 1 ? 0 : a.kv_heads * (int64_t)a.tiles * a.n_split * seq_part_floats(rows, head_dim) * 4;
+  const int64_t units = a.kv_heads * (int64_t)a.tiles;
+  return a.n_split == 1 ? 0 : units * 16 + units * a.n_split * seq_part_floats(rows, head_dim) * 4;
+}
+
+void use_workspace(SeqArgs &a, void *p) {
+  a.head = (int32_t *)p;
+  a.part = (float *)((char *)p + a.kv_heads * (int64_t)a.tiles * 16);
 }
 
 // --- packed attention -----------------------------------------------------------------
@@ -144,10 +158,10 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
   if (rows > INT32_MAX - kSeqRows || !good_grid(tiles * a.kv_heads))
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
-  a.n_split = choose_split(tiles * a.kv_heads, p->n_keys / p->n_seqs, 512, 8, kSeqMaxSplit);
+  choose_split(a, p->n_keys / p->n_seqs, 512, 8, kSeqMaxSplit);
   // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
-  a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24;
-  if (!good_grid(tiles * a.kv_heads * a.n_split)) a.n_split = 1;
+  a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24 &&
+           wide_rows(a, p->n_keys / p->n_seqs);
   return HC_OK;
 }
 
@@ -226,10 +240,12 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
   const int64_t keys = p->max_kv > 0 ? std::min(p->max_kv, k->capacity) : k->capacity;
-  a.n_split = choose_split(tiles * a.kv_heads, keys, few_rows ? 1024 : 512, few_rows ? 4 : 8,
-                           few_rows ? kDecodeMaxSplit : kSeqMaxSplit);
-  a.wide = k->head_dim == 128;
-  if (!good_grid(tiles * a.kv_heads * a.n_split)) a.n_split = 1;
+  // Single tokens: two work groups per CU read one long sequence fastest (131072 tokens of 8 heads: 26 us,
+  // 30 with four, 33 with eight); sequences of different lengths want more and shorter
+  // ranges (48 of them up to 8192: 31 us with 512 groups, 23 with 1024, 19 with 1536 and 2048).
+  if (few_rows) choose_split(a, keys, k->n_seqs == 1 ? 512 : 1536, 4, kDecodeMaxSplit);
+  else choose_split(a, keys, 512, 8, kSeqMaxSplit);
+  a.wide = k->head_dim == 128 && wide_rows(a, keys);
   return HC_OK;
 }
 
@@ -329,7 +345,7 @@ hc_status hc_packed_attention(hc_ctx *c, const hc_packed_args *p, hc_stream stre
   }
   if ((st = check_workspace(c, p->workspace, p->workspace_bytes, part_bytes(a, p->head_dim, kSeqRows))) != HC_OK)
     return st;
-  a.part = (float *)p->workspace;
+  if (a.n_split > 1) use_workspace(a, p->workspace);
   OnDevice on(c->device);
   HC_HIP(c, on.status);
   return run_seq(c, a, p->head_dim, false, (hipStream_t)stream);
@@ -377,7 +393,7 @@ hc_status hc_qcache_attention(hc_ctx *c, const hc_qcache *k, const hc_qcache_att
   if ((st = check_workspace(c, p->workspace, p->workspace_bytes,
                             part_bytes(a, k->head_dim, few_rows ? kDecodeRows : kSeqRows))) != HC_OK)
     return st;
-  a.part = (float *)p->workspace;
+  if (a.n_split > 1) use_workspace(a, p->workspace);
   OnDevice on(c->device);
   HC_HIP(c, on.status);
   return run_seq(c, a, k->head_dim, few_rows, (hipStream_t)stream);

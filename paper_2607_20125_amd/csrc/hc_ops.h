@@ -59,7 +59,7 @@ hipError_t launch_qcache_read(const QCacheArgs &a, hipStream_t s);
 // The rows of a (sequence, key head) are its queries times the query heads of that key
 // head: row r is query r / group, head r % group.  A unit is a run of kSeqRows of them
 // (kDecodeRows in the kernel for few rows), and each unit's key tiles may be cut into
-// n_split ranges whose partial results a second launch merges.
+// ranges whose partial results a second launch merges.
 constexpr int kSeqRows = 128, kDecodeRows = 16, kSeqKeys = 64;
 constexpr int kSeqMaxSplit = 32, kDecodeMaxSplit = 256;
 struct SeqArgs {
@@ -76,8 +76,9 @@ struct SeqArgs {
   int32_t kv_heads, group;
   int32_t block;                 // 0: every key is seen
   int32_t tiles;                 // units of a key head that the launch has room for
-  int32_t n_split;
-  float *part;                   // [kv_heads * tiles][n_split][rows (d + 2)]
+  int32_t n_split;               // key ranges of a unit
+  int32_t *head;                 // n_split > 1: [tiles][kv_heads][4], a unit's q0, row0, rows (0: none)
+  float *part;                   // [tiles][kv_heads][n_split][rows (d + 2)]
   float scale_log2;              // softmax scale * log2(e)
   bool wide;                     // 128-dim heads: waves of 64 rows (hc_seq128.hip)
 };

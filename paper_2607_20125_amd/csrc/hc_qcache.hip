@@ -90,44 +90,95 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
   return (uint32_t)min(max(e, kScaleLow), kScaleHigh);
 }
 
+// The 8x8 matrix of 2-byte elements that 8 neighbouring lanes hold (lane r: row r in four words)
+// transposed (lane c: column c), in three exchanges with the lanes 4, 2 and 1 away: halves
+// of 4, 2 and 1 elements change places.
+__device__ __forceinline__ u32x4 transpose8(u32x4 w) {
+  const int lane = threadIdx.x & 7;
+  auto from = [](uint32_t x, int d) { return (uint32_t)__shfl_xor((int)x, d); };
+  {
+    const bool up = lane & 4;          // keeps words 2, 3 and gives away 0, 1
+    const uint32_t g0 = from(up ? w[0] : w[2], 4), g1 = from(up ? w[1] : w[3], 4);
+    w = up ? u32x4{g0, g1, w[2], w[3]} : u32x4{w[0], w[1], g0, g1};
+  }
+  {
+    const bool up = lane & 2;
+    const uint32_t g0 = from(up ? w[0] : w[1], 2), g1 = from(up ? w[2] : w[3], 2);
+    w = up ? u32x4{g0, w[1], g1, w[3]} : u32x4{w[0], g0, w[2], g1};
+  }
+  const bool up = lane & 1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i], g = from(x, 1);
+    // even lane: (x low, g low); odd lane: (g high, x high)
+    w[i] = up ? __builtin_amdgcn_perm(x, g, 0x07060302u) : __builtin_amdgcn_perm(g, x, 0x05040100u);
+  }
+  return w;
+}
+
+// Whether the 8 lanes of a row of 8 hold the 8 tokens of one group of the cache's tiles: then their V
+// codes make 8 whole pieces of 16 bytes, one for each lane after a transposition.
+__device__ __forceinline__ bool whole_group(const Place &p) {
+  const uint64_t good = __ballot(p.ok && p.at % 8 == (int)(threadIdx.x & 7));
+  const int first = (threadIdx.x & 63) & ~7;
+  // (lanes whose tokens are the right ones of different groups belong to different tiles or
+  // sequences; then their row numbers do not continue their slots)
+  const uint64_t base = (uint64_t)(uintptr_t)p.tile + (uint64_t)(p.at / 8);
+  const uint32_t lo = (uint32_t)base, hi = (uint32_t)(base >> 32);
+  const int src = first;
+  const bool same = lo == (uint32_t)__shfl((int)lo, src) && hi == (uint32_t)__shfl((int)hi, src);
+  const uint64_t alike = __ballot(same);
+  return ((good & alike) >> first & 0xffu) == 0xffu;
+}
+
 template <int D>
 __global__ __launch_bounds__(kThreads) void qcache_append_kernel(QCacheArgs a) {
   const Place p = place<D>(a);
-  if (!p.ok) return;
-  const uint16_t *src = p.is_v ? (const uint16_t *)a.rows.v + p.row * a.rows.v_token + p.head * a.rows.v_head
-                               : (const uint16_t *)a.rows.k + p.row * a.rows.k_token + p.head * a.rows.k_head;
-  u32x4 w[4];
+  u32x4 c = {0, 0, 0, 0};
+  uint32_t code = 0;
+  if (p.ok) {
+    const uint16_t *src = p.is_v ? (const uint16_t *)a.rows.v + p.row * a.rows.v_token + p.head * a.rows.v_head
+                                 : (const uint16_t *)a.rows.k + p.row * a.rows.k_token + p.head * a.rows.k_head;
+    u32x4 w[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = gld16(src + p.grp * kQGroup + 8 * i);
-  uint32_t top = 0;
+    for (int i = 0; i < 4; ++i) w[i] = gld16(src + p.grp * kQGroup + 8 * i);
+    uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      top = max(top, max(w[i][j] << 16 & 0x7fffffffu, w[i][j] & 0x7fff0000u));
-  const uint32_t code = scale_code(top);
-  // the conversion divides by the scale, rounds to even and saturates at 6
-  const float scale = __uint_as_float(min(code, (uint32_t)kScaleHigh) << 23);
-  u32x4 c;
+      for (int j = 0; j < 4; ++j)
+        top = max(top, max(w[i][j] << 16 & 0x7fffffffu, w[i][j] & 0x7fff0000u));
+    code = scale_code(top);
+    // the conversion divides by the scale, rounds to even and saturates at 6
+    const float scale = __uint_as_float(min(code, (uint32_t)kScaleHigh) << 23);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w0 = w[i][0], w1 = w[i][1], w2 = w[i][2], w3 = w[i][3];
-    uint32_t r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w0), scale, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w1), scale, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w2), scale, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w3), scale, 3);
-    c[i] = r;
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w0 = w[i][0], w1 = w[i][1], w2 = w[i][2], w3 = w[i][3];
+      uint32_t r = 0;
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w0), scale, 0);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w1), scale, 1);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w2), scale, 2);
+      r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w3), scale, 3);
+      c[i] = r;
+    }
   }
+  // (K and V alternate by runs of 8 lanes and more, so a run of 8 is of one kind)
+  const bool whole = whole_group(p) && p.is_v;
+  const u32x4 turned = transpose8(c);
+  if (!p.ok) return;
   uint8_t *to = codes_at<D>(p);
-  if (p.is_v) {
+  if (!p.is_v) {
+    *(u32x4 *)to = c;
+  } else if (whole) {
+    // lane l has piece l (4 dims) of the 8 tokens; `to` is piece 0 of token l
+    const int l = threadIdx.x & 7;
+    *(u32x4 *)(to - 2 * l + 16 * l) = turned;
+  } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       *(uint16_t *)(to + 32 * i) = (uint16_t)c[i];
       *(uint16_t *)(to + 32 * i + 16) = (uint16_t)(c[i] >> 16);
     }
-  } else {
-    *(u32x4 *)to = c;
   }
   *scale_at<D>(p) = (uint8_t)code;
 }
@@ -135,16 +186,24 @@ __global__ __launch_bounds__(kThreads) void qcache_append_kernel(QCacheArgs a) {
 template <int D>
 __global__ __launch_bounds__(kThreads) void qcache_read_kernel(QCacheArgs a) {
   const Place p = place<D>(a);
-  if (!p.ok) return;
-  const uint8_t *from = codes_at<D>(p);
-  u32x4 c;
-  if (p.is_v) {
+  const bool whole = whole_group(p) && p.is_v;
+  u32x4 c = {0, 0, 0, 0};
+  if (p.ok) {
+    const uint8_t *from = codes_at<D>(p);
+    if (!p.is_v) {
+      c = *(const u32x4 *)from;
+    } else if (whole) {
+      const int l = threadIdx.x & 7;
+      c = *(const u32x4 *)(from - 2 * l + 16 * l);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      c[i] = *(const uint16_t *)(from + 32 * i) | (uint32_t) * (const uint16_t *)(from + 32 * i + 16) << 16;
-  } else {
-    c = *(const u32x4 *)from;
+      for (int i = 0; i < 4; ++i)
+        c[i] = *(const uint16_t *)(from + 32 * i) | (uint32_t) * (const uint16_t *)(from + 32 * i + 16) << 16;
+    }
   }
+  const u32x4 turned = transpose8(c);
+  if (!p.ok) return;
+  if (whole) c = turned;
   const float scale = __uint_as_float((uint32_t)*scale_at<D>(p) << 23);
   uint16_t *dst = p.is_v ? (uint16_t *)a.rows.v + p.row * a.rows.v_token + p.head * a.rows.v_head
                          : (uint16_t *)a.rows.k + p.row * a.rows.k_token + p.head * a.rows.k_head;

@@ -29,32 +29,74 @@ struct SeqUnit {
   int64_t q0, k0;          // first query and key of the sequence in the packed tensors
 };
 
+// Queries and keys of sequence s, clamped to the tensors.
+struct SeqSpan {
+  int q0, nq, k0, nk;
+};
+__device__ __forceinline__ SeqSpan seq_span(const SeqArgs &a, int s) {
+  SeqSpan p;
+  if (a.cu_q) {
+    p.q0 = min(max(a.cu_q[s], 0), a.n_tokens);
+    p.nq = max(min(a.cu_q[s + 1], a.n_tokens) - p.q0, 0);
+  } else {
+    p.nq = a.n_tokens / a.n_seqs;
+    p.q0 = s * p.nq;
+  }
+  if (a.kv_len) {
+    p.k0 = 0;
+    p.nk = min(max(a.kv_len[s], 0), a.capacity);
+  } else if (a.cu_k) {
+    p.k0 = min(max(a.cu_k[s], 0), a.n_keys);
+    p.nk = max(min(a.cu_k[s + 1], a.n_keys) - p.k0, 0);
+  } else {
+    p.k0 = p.q0;
+    p.nk = p.nq;
+  }
+  return p;
+}
+
 // Unit `tile` of the launch, in units of R rows; false if there is none.  Called by
-// whole waves.  Later units of a sequence come first: with a causal mask they have the most keys,
-// and work groups start in launch order.  Offsets are clamped to the tensors.
+// whole waves; results are uniform.  Work groups start in launch order, so what takes longest comes
+// first: the later units of a sequence, which see the most keys under a causal mask, before the
+// earlier ones, and up to 32 sequences by their keys.  (Ranking costs some 20 vector
+// instructions a sequence and wave.  With units of 16 rows, whose waves share a SIMD by
+// four, that was 5 us a work group for 48 sequences; there they stay in order.)
 template <int R>
 __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u) {
+  SeqSpan p;
   int units, j;
-  if (a.cu_q == nullptr) {
-    u.nq = a.n_tokens / a.n_seqs;
-    units = (u.nq * a.group + R - 1) / R;
-    u.seq = tile / units;
-    j = tile - u.seq * units;
-    u.q0 = (int64_t)u.seq * u.nq;
-    if (u.seq >= a.n_seqs) return false;
+  auto uniform = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };
+  if (a.n_seqs == 1) {
+    p = seq_span(a, 0);
+    units = (p.nq * a.group + R - 1) / R;
+    j = tile;
+    u.seq = 0;
+    if (j >= units) return false;
+  } else if (R == kSeqRows && a.n_seqs <= 32) {
+    // every lane takes a sequence and counts the units of those before it
+    const int lane = threadIdx.x & 63;
+    p = SeqSpan{0, 0, 0, 0};
+    if (lane < a.n_seqs) p = seq_span(a, lane);
+    const int mine = (p.nq * a.group + R - 1) / R;
+    int64_t before = 0;
+    for (int s = 0; s < a.n_seqs; ++s) {
+      const int keys = uniform(p.nk, s), n = uniform(mine, s);
+      if (keys > p.nk || (keys == p.nk && s < lane)) before += n;
+    }
+    const uint64_t here = __ballot(before <= tile && tile < before + mine);
+    if (here == 0) return false;
+    u.seq = __ffsll((unsigned long long)here) - 1;
+    units = mine;
+    j = (int)(tile - before);
   } else {
-    // every lane takes a sequence: a running count of units finds the one that holds `tile`
+    // in their order: a running count of units finds the one that holds `tile`
     const int lane = threadIdx.x & 63;
     int64_t before = 0;
     bool found = false;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-      const int s = s0 + lane;
-      int first = 0, n = 0;
-      if (s < a.n_seqs) {
-        first = min(max(a.cu_q[s], 0), a.n_tokens);
-        n = max(min(a.cu_q[s + 1], a.n_tokens) - first, 0);
-      }
-      const int mine = (n * a.group + R - 1) / R;
+      p = SeqSpan{0, 0, 0, 0};
+      if (s0 + lane < a.n_seqs) p = seq_span(a, s0 + lane);
+      const int mine = (p.nq * a.group + R - 1) / R;
       int upto = mine;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
@@ -63,38 +105,25 @@ __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u)
       }
       const uint64_t past = __ballot(before + upto > tile);
       if (past) {
-        const int l = __ffsll((unsigned long long)past) - 1;
-        u.seq = s0 + l;
-        u.nq = __shfl(n, l);
-        u.q0 = __shfl(first, l);
-        units = __shfl(mine, l);
-        j = (int)(tile - before) - (__shfl(upto, l) - units);
+        u.seq = s0 + __ffsll((unsigned long long)past) - 1;
+        units = mine;
+        j = (int)(tile - before) - (upto - mine);
         found = true;
         break;
       }
-      before += __shfl(upto, 63);
+      before += uniform(upto, 63);
     }
     if (!found) return false;
   }
+  const int l = __builtin_amdgcn_readfirstlane(u.seq % 64);
   u.seq = __builtin_amdgcn_readfirstlane(u.seq);
-  u.nq = __builtin_amdgcn_readfirstlane(u.nq);
-  u.q0 = __builtin_amdgcn_readfirstlane((int)u.q0);
+  const int from = a.n_seqs == 1 ? 0 : l;
+  u.nq = uniform(p.nq, from);
+  u.q0 = uniform(p.q0, from);
+  u.nk = uniform(p.nk, from);
+  u.k0 = uniform(p.k0, from);
   u.rows = u.nq * a.group;
-  u.row0 = __builtin_amdgcn_readfirstlane((units - 1 - j) * R);
-  if (a.kv_len) {
-    u.nk = min(max(a.kv_len[u.seq], 0), a.capacity);
-    u.k0 = 0;
-  } else if (a.cu_k) {
-    const int first = min(max(a.cu_k[u.seq], 0), a.n_keys);
-    u.k0 = first;
-    u.nk = max(min(a.cu_k[u.seq + 1], a.n_keys) - first, 0);
-  } else {
-    u.k0 = u.q0;
-    u.nk = u.nq;
-  }
-  // (loads from memory that the kernel might write: uniform all the same)
-  u.k0 = __builtin_amdgcn_readfirstlane((int)u.k0);
-  u.nk = __builtin_amdgcn_readfirstlane(u.nk);
+  u.row0 = (uniform(units, from) - 1 - uniform(j, from)) * R;
   return true;
 }
 
@@ -107,6 +136,65 @@ __device__ __forceinline__ int seen_keys(const SeqArgs &a, const SeqUnit &u, int
   const uint32_t end = ((uint32_t)p / (uint32_t)a.block + 1) * (uint32_t)a.block;
   return (int)min(end, (uint32_t)u.nk);
 }
+
+// The range of key tiles that a work group takes of its unit: [t0, t1) of the nt that any row
+// sees.  Where ranges are merged, the unit's place is left for that launch, which then need
+// not find it again.  (Ranges of one length for every unit, more of them for longer sequences, give work
+// groups that are alike but more that find nothing to do: 22.5 us instead of 18.9 for 48
+// sequences of 1 to 8192 cached tokens.)
+__device__ __forceinline__ void key_range(const SeqArgs &a, const SeqUnit &u, int tile, int head, int split, int nt,
+                                          int &t0, int &t1) {
+  t0 = (int)((int64_t)nt * split / a.n_split);
+  t1 = (int)((int64_t)nt * (split + 1) / a.n_split);
+  if (a.n_split > 1 && split == 0 && threadIdx.x == 0) {
+    int32_t *h = a.head + ((int64_t)tile * a.kv_heads + head) * 4;
+    h[0] = (int)u.q0;
+    h[1] = u.row0;
+    h[2] = u.rows;
+  }
+}
+// The same unit in the merge.
+__device__ __forceinline__ bool left_unit(const SeqArgs &a, int tile, int head, SeqUnit &u) {
+  const int32_t *h = a.head + ((int64_t)tile * a.kv_heads + head) * 4;
+  u.q0 = h[0];
+  u.row0 = h[1];
+  u.rows = h[2];
+  return u.rows > 0;
+}
+// A unit that does not exist says so to the merge.
+__device__ __forceinline__ void no_unit(const SeqArgs &a, int tile, int head, int split) {
+  if (a.n_split > 1 && split == 0 && threadIdx.x == 0) a.head[((int64_t)tile * a.kv_heads + head) * 4 + 2] = 0;
+}
+
+// 32 finished rows of a wave on their way to memory: a lane of the matrix layout holds 4 dims of
+// a row, which alone would be written 16 bytes of a row at a time; through LDS a row leaves
+// in one piece.  Piece p of row r (8 bytes) is kept at p ^ 2 (r % 16).
+template <int D>
+struct OutRows {
+  uint16_t *buf;                 // [32][D] of this wave's own
+  __device__ __forceinline__ explicit OutRows(uint16_t *b) : buf(b) {}
+  __device__ __forceinline__ void put(int r, int piece, float x0, float x1, float x2, float x3) {
+    const bf16x2 x = {(__bf16)x0, (__bf16)x1}, y = {(__bf16)x2, (__bf16)x3};
+    uint2 w;
+    w.x = __builtin_bit_cast(uint32_t, x);
+    w.y = __builtin_bit_cast(uint32_t, y);
+    *reinterpret_cast<uint2 *>(buf + r * D + (piece ^ (2 * (r % (D / 8)))) * 4) = w;
+  }
+  // rows `first` .. first + 31 of the unit
+  __device__ __forceinline__ void store(const SeqArgs &a, const SeqUnit &u, int head, int first, int lane) {
+    constexpr int C = D / 8;     // 16-byte chunks of a row
+#pragma unroll
+    for (int i = 0; i < 32 * C / 64; ++i) {
+      const int r = i * (64 / C) + lane / C, c = lane % C;
+      const int row = u.row0 + first + r;
+      const u32x4 w = *reinterpret_cast<const u32x4 *>(buf + r * D + (c ^ (r % C)) * 8);
+      if (row < u.rows) {
+        const int qi = row / a.group, qh = head * a.group + (row - qi * a.group);
+        *reinterpret_cast<u32x4 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + c * 8) = w;
+      }
+    }
+  }
+};
 
 }  // namespace dev
 }  // namespace hc

@@ -28,12 +28,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int split = rest % a.n_split, tile = rest / a.n_split;
   SeqUnit u;
-  if (!seq_unit<kSeqRows>(a, tile, u)) return;
+  if (!seq_unit<kSeqRows>(a, tile, u)) return no_unit(a, tile, head, split);
 
   // this lane's row, and its query and head
   const int row = u.row0 + wave * 32 + n;
-  const bool valid = row < u.rows;
-  const int at = valid ? row : u.rows - 1;
+  const int at = min(row, u.rows - 1);
   const int qi = at / a.group, qh = head * a.group + (at - qi * a.group);
   bf16x8 qf[NKK];
   {
@@ -46,8 +45,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   const int first = u.row0 / a.group, last = min(u.row0 + kSeqRows, u.rows) - 1;
   const int lo_all = seen_keys(a, u, first), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
-  const int t0 = (int)((int64_t)nt_all * split / a.n_split);
-  const int t1 = (int)((int64_t)nt_all * (split + 1) / a.n_split);
+  int t0, t1;
+  key_range(a, u, tile, head, split, nt_all, t0, t1);
   const float sl2 = a.scale_log2;
 
   // --- tiles ---------------------------------------------------------------------
@@ -237,20 +236,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
 
   const float l_tot = sum_xor32(l_run);
   if (a.n_split == 1) {
-    if (!valid) return;
     const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
-    uint16_t *op = a.o + (u.q0 + qi) * a.o_token + qh * a.o_head;
+    __syncthreads();              // every wave is done with the tiles
+    OutRows<D> out(&sK[0][0] + wave * 32 * D);
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
-      for (int rq = 0; rq < 4; ++rq) {
-        uint2 w;
-        const bf16x2 x = {(__bf16)(acc[db][4 * rq] * inv), (__bf16)(acc[db][4 * rq + 1] * inv)};
-        const bf16x2 y = {(__bf16)(acc[db][4 * rq + 2] * inv), (__bf16)(acc[db][4 * rq + 3] * inv)};
-        w.x = __builtin_bit_cast(uint32_t, x);
-        w.y = __builtin_bit_cast(uint32_t, y);
-        *reinterpret_cast<uint2 *>(op + 32 * db + 8 * rq + 4 * g) = w;
-      }
+      for (int rq = 0; rq < 4; ++rq)
+        out.put(n, 8 * db + 2 * rq + g, acc[db][4 * rq] * inv, acc[db][4 * rq + 1] * inv, acc[db][4 * rq + 2] * inv,
+                acc[db][4 * rq + 3] * inv);
+    out.store(a, u, head, wave * 32, lane);
   } else {
     const int lrow = wave * 32 + n;
     float *pp = a.part + (((int64_t)tile * a.kv_heads + head) * a.n_split + split) * seq_part_floats(kSeqRows, D);
@@ -279,7 +274,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int tile = rest / RP;
   SeqUnit u;
-  if (!seq_unit<R>(a, tile, u)) return;
+  if (!left_unit(a, tile, head, u)) return;
   const int lrow = (rest % RP) * RW + threadIdx.x / TR, row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int dim = threadIdx.x % TR * 4;
@@ -313,7 +308,7 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
   const int tile = rest / R, lrow = rest % R;
   SeqUnit u;
-  if (!seq_unit<R>(a, tile, u)) return;
+  if (!left_unit(a, tile, head, u)) return;
   const int row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;

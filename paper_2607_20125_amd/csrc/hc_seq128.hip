@@ -72,6 +72,14 @@ __device__ __forceinline__ void lds_dma16_bases(const uint16_t *base, int64_t st
       : "memory");
 }
 
+// A pointer that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ const uint16_t *uniform_ptr(const uint16_t *p) {
+  const uint64_t x = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (const uint16_t *)((uint64_t)hi << 32 | lo);
+}
+
 template <bool QUANT>
 __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   constexpr int D = 128, NQB = 2, KT = kSeqKeys, NKK = D / 16, NDB = D / 32;
@@ -84,10 +92,14 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int split = rest % a.n_split, tile = rest / a.n_split;
+  // (uniform values are kept in scalar registers, as the bases of the copies have to be;
+  // quotients come out of vector ones)
+  const int rest = __builtin_amdgcn_readfirstlane(blockIdx.x / a.kv_heads);
+  const int head = blockIdx.x - rest * a.kv_heads;
+  const int tile = __builtin_amdgcn_readfirstlane(rest / a.n_split);
+  const int split = rest - tile * a.n_split;
   SeqUnit u;
-  if (!seq_unit<kSeqRows>(a, tile, u)) return;
+  if (!seq_unit<kSeqRows>(a, tile, u)) return no_unit(a, tile, head, split);
 
   // this lane's rows wave 64 + 32 qb + n of the unit; a row behind the last repeats it
   int hi[NQB];               // keys it sees
@@ -101,7 +113,8 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) qf[qb][kk] = ld_g16(qp + 16 * kk + 8 * g);
   }
-  // Q in its registers before any DMA is issued (the compiler cannot count the DMAs)
+  // Q in its registers before any DMA is issued (issued behind it, the copies of the first
+  // tiles would be waited for with it: 3% slower where key ranges are short)
   wait_vmcnt<0>();
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb)
@@ -110,13 +123,14 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   const float sl2 = a.scale_log2;
 
   // The key range: nt tiles from tile t0 on.  Tiles below `plain` are seen whole by every row
-  // (seen_keys grows with the query), tile `ragged` holds the sequence's end.
+  // (seen_keys grows with the query).
   const int last = min(u.row0 + kSeqRows, u.rows) - 1;
   const int lo_all = seen_keys(a, u, u.row0 / a.group), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
-  // (in scalar registers, as the bases of the copies have to be)
-  const int t0 = __builtin_amdgcn_readfirstlane((int)((int64_t)nt_all * split / a.n_split));
-  const int nt = __builtin_amdgcn_readfirstlane((int)((int64_t)nt_all * (split + 1) / a.n_split) - t0);
+  int t0, t1;
+  key_range(a, u, tile, head, split, nt_all, t0, t1);
+  t0 = __builtin_amdgcn_readfirstlane(t0);
+  const int nt = __builtin_amdgcn_readfirstlane(t1 - t0);
   const int plain = __builtin_amdgcn_readfirstlane(lo_all / KT - t0);
   const int nk = u.nk - t0 * KT;             // keys of the sequence from tile t0 on
 
@@ -140,8 +154,8 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   auto k_chunk = [&](int j) { return kswz<D>(4 * (8 * wave + j) + dma_row, dma_pos); };
   const int v_chunk = dma_pos ^ (4 * dma_row);
   if constexpr (!QUANT) {
-    kbase = a.k + (u.k0 + (int64_t)t0 * KT) * a.k_token + head * a.k_head;
-    vbase = a.v + (u.k0 + (int64_t)t0 * KT) * a.v_token + head * a.v_head;
+    kbase = uniform_ptr(a.k + (u.k0 + (int64_t)t0 * KT) * a.k_token + head * a.k_head);
+    vbase = uniform_ptr(a.v + (u.k0 + (int64_t)t0 * KT) * a.v_token + head * a.v_head);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       ka[j] = (uint32_t)k_key(j) * (uint32_t)a.k_token * 2u + (uint32_t)(k_chunk(j) * 16 + 8192 - 1024 * j);
@@ -365,7 +379,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   };
   // S(t+1), then PV(t), with the probabilities of tile t from pair kPre on and the
   // first kPre pairs of tile t+1 beside the products.  STEADY: tile t+4 exists, tile t+1 is
-  // seen whole, kslot and nslot are constants, and kf holds the first reads of K(t+1).
+  // seen whole, kslot is a constant, and kf holds the first reads of K(t+1).
   auto step = [&](auto steady, int t, uint32_t kslot, Scores &cur, Scores &nxt, Probs &pf) {
     constexpr bool STEADY = decltype(steady)::value;
     const uint32_t vb = v_slot(t), vn = v_slot(t + 1);
@@ -631,29 +645,24 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     }
     if (any_fallback) run_max();
   }
+  __syncthreads();                // every wave is done with the tiles
 
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb) {
-    const int lrow = wave * 64 + qb * 32 + n, row = u.row0 + lrow;
+    const int lrow = wave * 64 + qb * 32 + n;
     // l_run: the row sum of this lane's row (the fixed-offset pass), or this
     // lane's half of it (the running-max pass)
     const float l_tot = any_fallback ? sum_xor32(l_run[qb]) : l_run[qb];
     if (a.n_split == 1) {
-      if (row >= u.rows) continue;
       const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
-      const int qi = row / a.group, qh = head * a.group + (row - qi * a.group);
-      uint16_t *op = a.o + (u.q0 + qi) * a.o_token + qh * a.o_head;
+      OutRows<D> out(&sV[0][0] + (wave * 2 + qb) * 32 * D);
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int rq = 0; rq < 4; ++rq) {
-          const bf16x2 x = {(__bf16)(acc[qb][db][4 * rq] * inv), (__bf16)(acc[qb][db][4 * rq + 1] * inv)};
-          const bf16x2 y = {(__bf16)(acc[qb][db][4 * rq + 2] * inv), (__bf16)(acc[qb][db][4 * rq + 3] * inv)};
-          uint2 w;
-          w.x = __builtin_bit_cast(uint32_t, x);
-          w.y = __builtin_bit_cast(uint32_t, y);
-          *reinterpret_cast<uint2 *>(op + 32 * db + 8 * rq + 4 * g) = w;
-        }
+        for (int rq = 0; rq < 4; ++rq)
+          out.put(n, 8 * db + 2 * rq + g, acc[qb][db][4 * rq] * inv, acc[qb][db][4 * rq + 1] * inv,
+                  acc[qb][db][4 * rq + 2] * inv, acc[qb][db][4 * rq + 3] * inv);
+      out.store(a, u, head, wave * 64 + qb * 32, lane);
     } else {
       float *pp = a.part + (((int64_t)tile * a.kv_heads + head) * a.n_split + split) * seq_part_floats(kSeqRows, D);
       float *op = pp + (int64_t)lrow * D;

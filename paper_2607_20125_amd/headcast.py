@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import numpy as np
 
@@ -117,8 +118,7 @@ def _load() -> ctypes.CDLL:
         "hc_profile_enable": (ctypes.c_int, [P, ctypes.c_int]),
         "hc_profile_read": (ctypes.c_int, [P, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                                            ctypes.POINTER(I64)]),
-        "hc_rotate": (ctypes.c_int, [P, ctypes.POINTER(HCRotateArgs),
-                                     ctypes.POINTER(HCRotateTensor), ctypes.c_int, P]),
+        "hc_rotate": (ctypes.c_int, [P, P, P, ctypes.c_int, P]),
         "hc_packed_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs),
                                                ctypes.POINTER(I64)]),
         "hc_packed_attention": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs), P]),
@@ -191,11 +191,34 @@ def _torch():
     return torch
 
 
-def _raw_stream(device):
-    """torch's current stream of a device as a hipStream_t (the short way where torch has it)."""
+@functools.lru_cache(maxsize=None)
+def _rotate_types():
+    return {_torch().bfloat16: BF16, _torch().float32: F32}
+
+
+@functools.lru_cache(maxsize=None)
+def _bf16():
+    return (_torch().bfloat16,)
+
+
+# The two structures of a rotation as native bytes: packing them costs a call a fifth of what filling
+# ctypes structures does, which counts where the kernel takes 4 us.
+_PACK_ROTATE = struct.Struct("@12i3idP").pack
+_PACK_TENSOR = {1: struct.Struct("@2P4qi4x").pack, 2: struct.Struct("@2P4qi4x2P4qi4x").pack}
+assert struct.calcsize("@12i3idP") == ctypes.sizeof(HCRotateArgs)
+assert struct.calcsize("@2P4qi4x") == ctypes.sizeof(HCRotateTensor)
+
+
+@functools.lru_cache(maxsize=None)
+def _raw_stream_of():
+    """torch's way to its current stream of a device as a hipStream_t (the short one if it is there)."""
     torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw else torch.cuda.current_stream(device).cuda_stream
+    return (getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            or (lambda device: torch.cuda.current_stream(device).cuda_stream))
+
+
+def _raw_stream(device):
+    return _raw_stream_of()(device)
 
 
 class QCache:
@@ -387,32 +410,35 @@ class Context:
         (bf16 or float32; `x` itself rotates in place), new ones by default.  Positions:
         int32 [axes][tokens], or the (frame, row, column) of the tokens of a `grid` of (height,
         width), the context's by default, from frame `frame0` on.  Returns `out`."""
-        torch = _torch()
         pair = isinstance(x, (tuple, list))
-        xs = list(x) if pair else [x]
+        xs = x if pair else (x,)
         if out is None:
-            outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
+            outs = tuple([_torch().empty(t.shape, dtype=t.dtype, device=t.device) for t in xs])
         else:
-            outs = list(out) if isinstance(out, (tuple, list)) else [out]
-        if len(outs) != len(xs) or not 1 <= len(xs) <= 2:
+            outs = out if isinstance(out, (tuple, list)) else (out,)
+        n_tensors, n_axes = len(xs), len(axis_dims)
+        if len(outs) != n_tensors or not 1 <= n_tensors <= 2:
             raise ValueError("rotate takes one tensor or a pair, and as many outputs")
-        if not 1 <= len(axis_dims) <= 4:
+        if not 1 <= n_axes <= 4:
             raise ValueError("axis_dims must have one to four entries")
-        types = {torch.bfloat16: BF16, torch.float32: F32}
-        n, d = xs[0].shape[0], xs[0].shape[-1]
-        tensors = (HCRotateTensor * len(xs))()
-        for i, (t, o) in enumerate(zip(xs, outs)):
-            if t.dtype != xs[0].dtype or o.dtype != outs[0].dtype:
-                raise ValueError("both tensors of a pair must have the same type")
-            xp, xt, xh = self._rows("x", t, types, None if i == 0 else (n, t.shape[1], d))
-            op, ot, oh = self._rows("out", o, types, t.shape)
-            tensors[i] = HCRotateTensor(xp, op, xt, xh, ot, oh, t.shape[1])
-        gh, gw = grid if grid is not None else (self.cfg.grid_h, self.cfg.grid_w)
-        a = HCRotateArgs(n, d, types[xs[0].dtype], types[outs[0].dtype], len(axis_dims),
-                         (_I32 * 4)(*axis_dims), bool(halves), bool(joint), bool(inverse), gh, gw, frame0,
-                         theta, self._ints("positions", positions, (len(axis_dims), n)))
-        self._check(lib.hc_rotate(self._h, ctypes.byref(a), tensors, len(xs), _raw_stream(self.device)),
-                    "hc_rotate")
+        types = _rotate_types()
+        n, _, d = xs[0].shape if xs[0].dim() == 3 else (0, 0, -1)
+        x_type, out_type = xs[0].dtype, outs[0].dtype
+        tensors = []
+        for t, o in zip(xs, outs):
+            shape = t.shape
+            if t.dtype is not x_type or o.dtype is not out_type or shape[0] != n or shape[-1] != d:
+                raise ValueError("a pair has the same tokens, dims and types")
+            xp, xt, xh = self._rows("x", t, types)
+            op, ot, oh = self._rows("out", o, types, shape)
+            tensors += xp, op, xt, xh, ot, oh, shape[1]
+        gh, gw = (self.cfg.grid_h, self.cfg.grid_w) if grid is None else grid
+        args = _PACK_ROTATE(n, d, types[x_type], types[out_type], n_axes, *axis_dims, *(0,) * (4 - n_axes),
+                            bool(halves), bool(joint), bool(inverse), gh, gw, frame0, theta,
+                            0 if positions is None else self._ints("positions", positions, (n_axes, n)))
+        status = lib.hc_rotate(self._h, args, _PACK_TENSOR[n_tensors](*tensors), n_tensors, _raw_stream(self.device))
+        if status:
+            self._check(status, "hc_rotate")
         return tuple(outs) if pair else outs[0]
 
     def packed_attention(self, q, k, v, cu_q=None, cu_k=None, out=None, *, causal_block=0,
@@ -420,25 +446,29 @@ class Context:
         """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
         cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
         None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
-        torch = _torch()
-        bf16 = (torch.bfloat16,)
+        bf16 = _bf16()
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
         if n_seqs is None:
             n_seqs = cu_q.shape[0] - 1 if cu_q is not None else 1
+        qs, ks = q.shape, k.shape
         qp, qt, qh = self._rows("q", q, bf16)
-        kp, kt, kh = self._rows("k", k, bf16, (k.shape[0], k.shape[1], q.shape[2]) if k.dim() == 3 else None)
-        vp, vt, vh = self._rows("v", v, bf16, k.shape)
-        op, ot, oh = self._rows("out", out, bf16, q.shape)
-        a = HCPackedArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, q.shape[0], k.shape[0], n_seqs,
-                         q.shape[1], k.shape[1], q.shape[2], causal_block, softmax_scale,
-                         self._ints("cu_q", cu_q, (n_seqs + 1,)), self._ints("cu_k", cu_k, (n_seqs + 1,)))
+        kp, kt, kh = self._rows("k", k, bf16)
+        vp, vt, vh = self._rows("v", v, bf16, ks)
+        op, ot, oh = self._rows("out", out, bf16, qs)
+        if ks[2] != qs[2]:
+            raise ValueError(f"k: expected heads of {qs[2]} dims, got {tuple(ks)}")
+        a = HCPackedArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, qs[0], ks[0], n_seqs, qs[1], ks[1], qs[2],
+                         causal_block, softmax_scale, self._ints("cu_q", cu_q, (n_seqs + 1,)),
+                         self._ints("cu_k", cu_k, (n_seqs + 1,)))
         need = ctypes.c_int64()
-        self._check(lib.hc_packed_workspace(self._h, ctypes.byref(a), ctypes.byref(need)),
-                    "hc_packed_workspace")
+        status = lib.hc_packed_workspace(self._h, a, need)
+        if status:
+            self._check(status, "hc_packed_workspace")
         held = self._work(a, need.value, workspace)
-        self._check(lib.hc_packed_attention(self._h, ctypes.byref(a), _raw_stream(self.device)),
-                    "hc_packed_attention")
+        status = lib.hc_packed_attention(self._h, a, _raw_stream(self.device))
+        if status:
+            self._check(status, "hc_packed_attention")
         del held
         return out
 
@@ -447,13 +477,14 @@ class Context:
         return QCache(n_seqs, n_heads, head_dim, capacity, f"cuda:{self.device}")
 
     def _cache_rows(self, fn, what, cache, k, v, start, cu_seqlens):
-        torch = _torch()
         shape = (k.shape[0], cache.n_heads, cache.head_dim)
-        kp, kt, kh = self._rows("k", k, (torch.bfloat16,), shape)
-        vp, vt, vh = self._rows("v", v, (torch.bfloat16,), shape)
+        kp, kt, kh = self._rows("k", k, _bf16(), shape)
+        vp, vt, vh = self._rows("v", v, _bf16(), shape)
         r = HCQCacheRows(kp, vp, kt, kh, vt, vh, shape[0], self._ints("start", start, (cache.n_seqs,)),
                          self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
-        self._check(fn(self._h, ctypes.byref(cache.desc), ctypes.byref(r), _raw_stream(self.device)), what)
+        status = fn(self._h, cache.desc, r, _raw_stream(self.device))
+        if status:
+            self._check(status, what)
 
     def qcache_append(self, cache: QCache, k, v, start, cu_seqlens=None):
         """hc_qcache_append: stores the rows of k and v (bf16 [tokens][cache heads][head_dim])
@@ -468,20 +499,24 @@ class Context:
                          causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
         """hc_qcache_attention: attention of q over the first kv_len[s] (int32 [n_seqs]) slots
         of each sequence of the cache.  Returns `out` (bf16, the shape of q)."""
-        torch = _torch()
+        bf16 = _bf16()
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qp, qt, qh = self._rows("q", q, (torch.bfloat16,),
-                                (q.shape[0], q.shape[1], cache.head_dim) if q.dim() == 3 else None)
-        op, ot, oh = self._rows("out", out, (torch.bfloat16,), q.shape)
-        a = HCQCacheAttentionArgs(qp, op, qt, qh, ot, oh, q.shape[0], q.shape[1], causal_block, max_kv,
-                                  softmax_scale, self._ints("kv_len", kv_len, (cache.n_seqs,)),
+            out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+        qs = q.shape
+        qp, qt, qh = self._rows("q", q, bf16)
+        op, ot, oh = self._rows("out", out, bf16, qs)
+        if qs[2] != cache.head_dim:
+            raise ValueError(f"q: expected heads of {cache.head_dim} dims, got {tuple(qs)}")
+        a = HCQCacheAttentionArgs(qp, op, qt, qh, ot, oh, qs[0], qs[1], causal_block, max_kv, softmax_scale,
+                                  self._ints("kv_len", kv_len, (cache.n_seqs,)),
                                   self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
         need = ctypes.c_int64()
-        self._check(lib.hc_qcache_workspace(self._h, ctypes.byref(cache.desc), ctypes.byref(a),
-                                            ctypes.byref(need)), "hc_qcache_workspace")
+        status = lib.hc_qcache_workspace(self._h, cache.desc, a, need)
+        if status:
+            self._check(status, "hc_qcache_workspace")
         held = self._work(a, need.value, workspace)
-        self._check(lib.hc_qcache_attention(self._h, ctypes.byref(cache.desc), ctypes.byref(a),
-                                            _raw_stream(self.device)), "hc_qcache_attention")
+        status = lib.hc_qcache_attention(self._h, cache.desc, a, _raw_stream(self.device))
+        if status:
+            self._check(status, "hc_qcache_attention")
         del held
         return out

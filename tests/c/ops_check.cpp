@@ -208,7 +208,7 @@ void packed_refusals() {
   CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_E_INVAL);
   p.workspace_bytes = bytes;
   CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_OK && merged && attended.n_split > 1);
-  CHECK(bytes == (int64_t)attended.kv_heads * attended.tiles * attended.n_split * 128 * (64 + 2) * 4);
+  CHECK(bytes == (int64_t)attended.kv_heads * attended.tiles * (16 + attended.n_split * 128 * (64 + 2) * 4));
   p.workspace = memory + 1028;
   CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_E_INVAL);
 }
