@@ -46,10 +46,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i = lane & 15, g = lane >> 4;
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int split = rest % a.n_split, tile = rest / a.n_split;
+  const SeqShare share = seq_share(a);
+  const int head = share.head;
   SeqUnit u;
-  if (!seq_unit<R>(a, tile, u)) return no_unit(a, tile, head, split);
+  if (!seq_unit<R>(a, share.tile, u)) return no_unit(share);
 
   const int at = min(u.row0 + i, u.rows - 1);
   const int qi = at / a.group, qh = head * a.group + (at - qi * a.group);
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
   const int lo_all = seen_keys(a, u, u.row0 / a.group), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
   int t0, t1;
-  key_range(a, u, tile, head, split, nt_all, t0, t1);
+  key_range(a, u, share, nt_all, t0, t1);
   const float sl2 = a.scale_log2;
   const uint8_t *base = a.cache + ((int64_t)u.seq * a.kv_heads + head) * a.cache_head;
 
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
     for (int e = 0; e < ND; ++e) o[e] += f * sO[w][row][dim + e];
   }
   if (u.row0 + row >= u.rows) return;
-  if (a.n_split == 1) {
+  if (!share.cut) {
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
     const int rq = (u.row0 + row) / a.group, rh = head * a.group + (u.row0 + row - rq * a.group);
     uint16_t *op = a.o + (u.q0 + rq) * a.o_token + rh * a.o_head + dim;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
       *reinterpret_cast<uint2 *>(op + e) = w;
     }
   } else {
-    float *pp = a.part + (((int64_t)tile * a.kv_heads + head) * a.n_split + split) * seq_part_floats(R, D);
+    float *pp = a.part + share.slot * seq_part_floats(R, D);
 #pragma unroll
     for (int e = 0; e < ND; e += 4)
       *reinterpret_cast<f32x4 *>(pp + row * D + dim + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
 }  // namespace
 
 hipError_t launch_decode(const SeqArgs &a, int head_dim, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * a.n_split)), block(64 * kWaves);
+  const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
   if (head_dim == 128) hipLaunchKernelGGL((decode_attn_kernel<128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((decode_attn_kernel<64>), grid, block, 0, s, a);
   return hipGetLastError();

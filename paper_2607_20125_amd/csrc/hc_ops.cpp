@@ -80,7 +80,7 @@ float scale_log2(float scale, int head_dim) {
 // Units of R rows that the sequences of a call can have: whole ones, and a partial one each
 // (exactly that many where all sequences are alike).
 int64_t unit_room(int64_t n_tokens, int64_t n_seqs, int64_t group, int R, bool alike) {
-  if (alike) return n_seqs * ((n_tokens / n_seqs * group + R - 1) / R);
+  if (alike || n_seqs == 1) return n_seqs * ((n_tokens / n_seqs * group + R - 1) / R);
   return n_tokens * group / R + std::min(n_seqs, n_tokens);
 }
 
@@ -101,6 +101,28 @@ bool wide_rows(const SeqArgs &a, int64_t keys) {
   return keys >= ((int64_t)a.tiles * a.kv_heads * a.n_split >= 256 ? 384 : 1536);
 }
 
+// Wide kernel, one sequence, no mask: all units take alike, and two work groups per CU make 512
+// places for them.  What is left over after whole rounds would run alone, each unit on a place of its
+// own; instead those units are cut so that their pieces fill the places again: 588 units
+// (6200 rows of 12 heads) over 32760 keys without this took as long as 1024 would.
+void cut_last_round(SeqArgs &a, int64_t keys) {
+  constexpr int64_t places = 512;
+  const int64_t units = seq_units(a), over = units % places;
+  if (!a.wide || a.n_split != 1 || a.n_seqs != 1 || a.block != 0 || units < places || over == 0) return;
+  const int64_t tiles = (keys + kSeqKeys - 1) / kSeqKeys;
+  // rounds of pieces, in units, and what a cut costs: about 8 tiles for the start and end of a
+  // piece and its partial result
+  auto cost = [&](int64_t p) {
+    return (double)((over * p + places - 1) / places) * (1.0 / p + (p > 1 ? 8.0 / tiles : 0.0));
+  };
+  int64_t best = 1;
+  for (int64_t p = 2; p <= 8; ++p)
+    if (cost(p) < cost(best)) best = p;
+  if (best == 1) return;
+  a.whole = (int32_t)(units - over);
+  a.n_split = (int32_t)best;
+}
+
 hc_status run_seq(hc_ctx *c, const SeqArgs &a, int head_dim, bool few_rows, hipStream_t s) {
   return timed_launch(c, s, HC_K_SEQUENCE, [&] {
     hipError_t e = few_rows ? launch_decode(a, head_dim, s) : launch_seq(a, head_dim, s);
@@ -118,13 +140,12 @@ hc_status check_workspace(hc_ctx *c, const void *p, int64_t bytes, int64_t neede
 }
 
 int64_t part_bytes(const SeqArgs &a, int head_dim, int rows) {
-  const int64_t units = a.kv_heads * (int64_t)a.tiles;
-  return a.n_split == 1 ? 0 : units * 16 + units * a.n_split * seq_part_floats(rows, head_dim) * 4;
+  return seq_cut_units(a) * (16 + a.n_split * seq_part_floats(rows, head_dim) * 4);
 }
 
 void use_workspace(SeqArgs &a, void *p) {
   a.head = (int32_t *)p;
-  a.part = (float *)((char *)p + a.kv_heads * (int64_t)a.tiles * 16);
+  a.part = (float *)((char *)p + seq_cut_units(a) * 16);
 }
 
 // --- packed attention -----------------------------------------------------------------
@@ -162,6 +183,7 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
   // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
   a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24 &&
            wide_rows(a, p->n_keys / p->n_seqs);
+  cut_last_round(a, p->n_keys);
   return HC_OK;
 }
 
@@ -198,7 +220,7 @@ hc_status cache_rows(hc_ctx *c, const hc_qcache *k, const hc_qcache_rows *r, boo
     if (st != HC_OK) return st;
   }
   if (!r->start || !aligned4(r->start)) return fail(c, HC_E_INVAL, "start must be a 4-byte aligned device pointer");
-  if (!good_grid(((int64_t)r->n_tokens + 7) / 8 * 8 * k->n_heads / 256 * 2 * (k->head_dim / kQGroup) + 1))
+  if (!good_grid(((int64_t)r->n_tokens + 7) / 8 * 8 * k->n_heads / 256 * 2 * (k->head_dim / 8) + 1))
     return fail(c, HC_E_INVAL, "too many rows for one call");
   OnDevice on(c->device);
   HC_HIP(c, on.status);
@@ -245,7 +267,8 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
   // ranges (48 of them up to 8192: 31 us with 512 groups, 23 with 1024, 19 with 1536 and 2048).
   if (few_rows) choose_split(a, keys, k->n_seqs == 1 ? 512 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);
-  a.wide = k->head_dim == 128 && wide_rows(a, keys);
+  a.wide = k->head_dim == 128 && !few_rows && wide_rows(a, keys);
+  cut_last_round(a, keys);
   return HC_OK;
 }
 

@@ -58,8 +58,8 @@ hipError_t launch_qcache_read(const QCacheArgs &a, hipStream_t s);
 // --- attention over sequences -------------------------------------------------------
 // The rows of a (sequence, key head) are its queries times the query heads of that key
 // head: row r is query r / group, head r % group.  A unit is a run of kSeqRows of them
-// (kDecodeRows in the kernel for few rows), and each unit's key tiles may be cut into
-// ranges whose partial results a second launch merges.
+// (kDecodeRows in the kernel for few rows), and units may be cut into key ranges whose
+// partial results a second launch merges.
 constexpr int kSeqRows = 128, kDecodeRows = 16, kSeqKeys = 64;
 constexpr int kSeqMaxSplit = 32, kDecodeMaxSplit = 256;
 struct SeqArgs {
@@ -76,12 +76,17 @@ struct SeqArgs {
   int32_t kv_heads, group;
   int32_t block;                 // 0: every key is seen
   int32_t tiles;                 // units of a key head that the launch has room for
-  int32_t n_split;               // key ranges of a unit
-  int32_t *head;                 // n_split > 1: [tiles][kv_heads][4], a unit's q0, row0, rows (0: none)
-  float *part;                   // [tiles][kv_heads][n_split][rows (d + 2)]
+  // Units, numbered tile * kv_heads + head: the first `whole` are one work group each, the others are cut
+  // into n_split key ranges, whose work groups come after those.
+  int32_t whole, n_split;
+  int32_t *head;                 // cut units: [unit - whole][4]: q0, row0, rows (0: no such unit)
+  float *part;                   // [unit - whole][n_split][rows (d + 2)]
   float scale_log2;              // softmax scale * log2(e)
   bool wide;                     // 128-dim heads: waves of 64 rows (hc_seq128.hip)
 };
+inline int64_t seq_units(const SeqArgs &a) { return (int64_t)a.tiles * a.kv_heads; }
+inline int64_t seq_cut_units(const SeqArgs &a) { return a.n_split > 1 ? seq_units(a) - a.whole : 0; }
+inline int64_t seq_groups(const SeqArgs &a) { return a.whole + (seq_units(a) - a.whole) * a.n_split; }
 // Floats of one partial result: rows of d sums, then the rows' maxima and sums.
 constexpr int64_t seq_part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
 hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s);

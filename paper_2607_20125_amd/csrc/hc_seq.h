@@ -137,33 +137,57 @@ __device__ __forceinline__ int seen_keys(const SeqArgs &a, const SeqUnit &u, int
   return (int)min(end, (uint32_t)u.nk);
 }
 
-// The range of key tiles that a work group takes of its unit: [t0, t1) of the nt that any row
-// sees.  Where ranges are merged, the unit's place is left for that launch, which then need
-// not find it again.  (Ranges of one length for every unit, more of them for longer sequences, give work
-// groups that are alike but more that find nothing to do: 22.5 us instead of 18.9 for 48
-// sequences of 1 to 8192 cached tokens.)
-__device__ __forceinline__ void key_range(const SeqArgs &a, const SeqUnit &u, int tile, int head, int split, int nt,
-                                          int &t0, int &t1) {
-  t0 = (int)((int64_t)nt * split / a.n_split);
-  t1 = (int)((int64_t)nt * (split + 1) / a.n_split);
-  if (a.n_split > 1 && split == 0 && threadIdx.x == 0) {
-    int32_t *h = a.head + ((int64_t)tile * a.kv_heads + head) * 4;
-    h[0] = (int)u.q0;
-    h[1] = u.row0;
-    h[2] = u.rows;
+// What a work group has of the units: one of them, whole or a range of its keys.
+struct SeqShare {
+  int tile, head, split;
+  bool cut;
+  int64_t slot;            // of its partial result
+  int32_t *place;          // where a cut unit's place is left for the merge
+};
+__device__ __forceinline__ SeqShare seq_share(const SeqArgs &a) {
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };    // (quotients come out of vector registers)
+  SeqShare s;
+  const int units = a.tiles * a.kv_heads, i = (int)blockIdx.x - a.whole;
+  int unit = (int)blockIdx.x;
+  s.split = 0;
+  s.cut = i >= 0 && a.n_split > 1;
+  if (i >= 0) {
+    s.split = uniform(i / (units - a.whole));
+    unit = a.whole + i - s.split * (units - a.whole);
+  }
+  s.tile = uniform(unit / a.kv_heads);
+  s.head = unit - s.tile * a.kv_heads;
+  s.slot = (int64_t)(unit - a.whole) * a.n_split + s.split;
+  s.place = a.head + (int64_t)(unit - a.whole) * 4;
+  return s;
+}
+// The range of key tiles that it takes: [t0, t1) of the nt that any row sees.  (Ranges of one length for
+// every unit, more of them for longer sequences, give work groups that are alike but more
+// that find nothing to do: 22.5 us instead of 18.9 for 48 sequences of 1 to 8192 cached tokens.)
+__device__ __forceinline__ void key_range(const SeqArgs &a, const SeqUnit &u, const SeqShare &s, int nt, int &t0, int &t1) {
+  t0 = 0;
+  t1 = nt;
+  if (!s.cut) return;
+  t0 = (int)((int64_t)nt * s.split / a.n_split);
+  t1 = (int)((int64_t)nt * (s.split + 1) / a.n_split);
+  if (s.split == 0 && threadIdx.x == 0) {
+    s.place[0] = (int)u.q0;
+    s.place[1] = u.row0;
+    s.place[2] = u.rows;
   }
 }
-// The same unit in the merge.
-__device__ __forceinline__ bool left_unit(const SeqArgs &a, int tile, int head, SeqUnit &u) {
-  const int32_t *h = a.head + ((int64_t)tile * a.kv_heads + head) * 4;
+// A unit that does not exist says so to the merge.
+__device__ __forceinline__ void no_unit(const SeqShare &s) {
+  if (s.cut && s.split == 0 && threadIdx.x == 0) s.place[2] = 0;
+}
+// Cut unit i in the merge.
+__device__ __forceinline__ bool left_unit(const SeqArgs &a, int i, SeqUnit &u, int &head) {
+  const int32_t *h = a.head + (int64_t)i * 4;
   u.q0 = h[0];
   u.row0 = h[1];
   u.rows = h[2];
+  head = (a.whole + i) % a.kv_heads;
   return u.rows > 0;
-}
-// A unit that does not exist says so to the merge.
-__device__ __forceinline__ void no_unit(const SeqArgs &a, int tile, int head, int split) {
-  if (a.n_split > 1 && split == 0 && threadIdx.x == 0) a.head[((int64_t)tile * a.kv_heads + head) * 4 + 2] = 0;
 }
 
 // 32 finished rows of a wave on their way to memory: a lane of the matrix layout holds 4 dims of

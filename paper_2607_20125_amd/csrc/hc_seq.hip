@@ -25,10 +25,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int split = rest % a.n_split, tile = rest / a.n_split;
+  const SeqShare share = seq_share(a);
+  const int head = share.head;
   SeqUnit u;
-  if (!seq_unit<kSeqRows>(a, tile, u)) return no_unit(a, tile, head, split);
+  if (!seq_unit<kSeqRows>(a, share.tile, u)) return no_unit(share);
 
   // this lane's row, and its query and head
   const int row = u.row0 + wave * 32 + n;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   const int lo_all = seen_keys(a, u, first), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
   int t0, t1;
-  key_range(a, u, tile, head, split, nt_all, t0, t1);
+  key_range(a, u, share, nt_all, t0, t1);
   const float sl2 = a.scale_log2;
 
   // --- tiles ---------------------------------------------------------------------
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   }
 
   const float l_tot = sum_xor32(l_run);
-  if (a.n_split == 1) {
+  if (!share.cut) {
     const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
     __syncthreads();              // every wave is done with the tiles
     OutRows<D> out(&sK[0][0] + wave * 32 * D);
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
     out.store(a, u, head, wave * 32, lane);
   } else {
     const int lrow = wave * 32 + n;
-    float *pp = a.part + (((int64_t)tile * a.kv_heads + head) * a.n_split + split) * seq_part_floats(kSeqRows, D);
+    float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
     float *op = pp + (int64_t)lrow * D;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -271,14 +271,14 @@ template <int D, int R>
 __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   constexpr int TR = D / 4, RW = 256 / TR, RP = R / RW;      // threads a row, rows a group, groups a unit
   static_assert(R % RW == 0, "rows of a unit");
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int tile = rest / RP;
+  const int unit = blockIdx.x / RP;
   SeqUnit u;
-  if (!left_unit(a, tile, head, u)) return;
-  const int lrow = (rest % RP) * RW + threadIdx.x / TR, row = u.row0 + lrow;
+  int head;
+  if (!left_unit(a, unit, u, head)) return;
+  const int lrow = (blockIdx.x % RP) * RW + threadIdx.x / TR, row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int dim = threadIdx.x % TR * 4;
-  const float *pp = a.part + ((int64_t)tile * a.kv_heads + head) * a.n_split * seq_part_floats(R, D);
+  const float *pp = a.part + (int64_t)unit * a.n_split * seq_part_floats(R, D);
   float M = kMInit;
   for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, pp[i * seq_part_floats(R, D) + R * D + lrow]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -305,14 +305,14 @@ template <int D, int R>
 __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   constexpr int TR = D / 4, NG = 256 / TR;
   __shared__ float sW[kDecodeMaxSplit], sL[kDecodeMaxSplit], sO[NG][D], sM[4];
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int tile = rest / R, lrow = rest % R;
+  const int unit = blockIdx.x / R, lrow = blockIdx.x % R;
   SeqUnit u;
-  if (!left_unit(a, tile, head, u)) return;
+  int head;
+  if (!left_unit(a, unit, u, head)) return;
   const int row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float *pp = a.part + ((int64_t)tile * a.kv_heads + head) * a.n_split * seq_part_floats(R, D);
+  const float *pp = a.part + (int64_t)unit * a.n_split * seq_part_floats(R, D);
   const float *ml = pp + tid * seq_part_floats(R, D) + R * D + lrow;
   const float m = tid < a.n_split ? ml[0] : kMInit;
   const float l = tid < a.n_split ? ml[R] : 0.f;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
 }  // namespace
 
 hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * a.n_split)), block(64 * kWaves);
+  const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
   if (head_dim == 128 && a.wide) return launch_seq128(a, s);
   if (head_dim == 128) {
     if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<128, true>), grid, block, 0, s, a);
@@ -366,7 +366,7 @@ hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
 hipError_t launch_seq_merge(const SeqArgs &a, int head_dim, int rows, hipStream_t s) {
   const bool many = a.n_split > 8;
   const int per = many ? rows : rows * head_dim / 1024;      // work groups of a unit
-  const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * per)), block(256);
+  const dim3 grid((uint32_t)(seq_cut_units(a) * per)), block(256);
 #define HC_MERGE(D, R)                                                                     \
   if (many) hipLaunchKernelGGL((seq_merge_many_kernel<D, R>), grid, block, 0, s, a);       \
   else hipLaunchKernelGGL((seq_merge_kernel<D, R>), grid, block, 0, s, a)

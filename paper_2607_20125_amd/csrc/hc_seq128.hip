@@ -92,14 +92,10 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
-  // (uniform values are kept in scalar registers, as the bases of the copies have to be;
-  // quotients come out of vector ones)
-  const int rest = __builtin_amdgcn_readfirstlane(blockIdx.x / a.kv_heads);
-  const int head = blockIdx.x - rest * a.kv_heads;
-  const int tile = __builtin_amdgcn_readfirstlane(rest / a.n_split);
-  const int split = rest - tile * a.n_split;
+  const SeqShare share = seq_share(a);
+  const int head = share.head;
   SeqUnit u;
-  if (!seq_unit<kSeqRows>(a, tile, u)) return no_unit(a, tile, head, split);
+  if (!seq_unit<kSeqRows>(a, share.tile, u)) return no_unit(share);
 
   // this lane's rows wave 64 + 32 qb + n of the unit; a row behind the last repeats it
   int hi[NQB];               // keys it sees
@@ -128,7 +124,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   const int lo_all = seen_keys(a, u, u.row0 / a.group), hi_all = seen_keys(a, u, last / a.group);
   const int nt_all = (hi_all + KT - 1) / KT;
   int t0, t1;
-  key_range(a, u, tile, head, split, nt_all, t0, t1);
+  key_range(a, u, share, nt_all, t0, t1);
   t0 = __builtin_amdgcn_readfirstlane(t0);
   const int nt = __builtin_amdgcn_readfirstlane(t1 - t0);
   const int plain = __builtin_amdgcn_readfirstlane(lo_all / KT - t0);
@@ -653,7 +649,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     // l_run: the row sum of this lane's row (the fixed-offset pass), or this
     // lane's half of it (the running-max pass)
     const float l_tot = any_fallback ? sum_xor32(l_run[qb]) : l_run[qb];
-    if (a.n_split == 1) {
+    if (!share.cut) {
       const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
       OutRows<D> out(&sV[0][0] + (wave * 2 + qb) * 32 * D);
 #pragma unroll
@@ -664,7 +660,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
                   acc[qb][db][4 * rq + 2] * inv, acc[qb][db][4 * rq + 3] * inv);
       out.store(a, u, head, wave * 64 + qb * 32, lane);
     } else {
-      float *pp = a.part + (((int64_t)tile * a.kv_heads + head) * a.n_split + split) * seq_part_floats(kSeqRows, D);
+      float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
       float *op = pp + (int64_t)lrow * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
@@ -683,7 +679,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
 }  // namespace
 
 hipError_t launch_seq128(const SeqArgs &a, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)a.tiles * a.kv_heads * a.n_split)), block(128);
+  const dim3 grid((uint32_t)seq_groups(a)), block(128);
   if (a.cache) hipLaunchKernelGGL((seq_attn128_kernel<true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((seq_attn128_kernel<false>), grid, block, 0, s, a);
   return hipGetLastError();

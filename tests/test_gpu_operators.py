@@ -258,6 +258,75 @@ def test_packed_attention(ctx, case):
     packed_case(ctx, case)
 
 
+# Long key ranges: every path of the kernels for 128-dim heads (the written-out steps, the look at the row
+# sums, tiles that not all rows see whole, ranges that share units evenly), against 64 bits on the GPU.
+LONG = [
+    # queries, keys, key heads, group, block
+    (1000, 5000, 4, 1, 0),
+    (2000, 2000, 8, 2, 1),
+    (1500, 3500, 6, 3, 700),
+    (4200, 8300, 9, 1, 0),           # 297 units on 512 places
+    (8000, 8200, 9, 1, 0),           # 567 units
+    (4096, 8192, 12, 1, 0),          # whole units only, 384 of them
+    (640, 9000, 3, 1, 1),
+]
+
+
+def long_reference(q, k, v, block, scale=None):
+    n, heads, d = q.shape
+    m, group = k.shape[0], heads // k.shape[1]
+    count = torch.tensor(R.seen(n, m, block), device="cuda").unsqueeze(1)
+    hidden = torch.arange(m, device="cuda") >= count
+    out, mag = [], []
+    for h in range(heads):
+        p = q[:, h].double() @ k[:, h // group].double().T * (scale if scale else d ** -0.5)
+        p = torch.softmax(p.masked_fill_(hidden, -math.inf), -1)
+        w = v[:, h // group].double()
+        out.append(p @ w)
+        mag.append(p @ w.abs())
+    return torch.stack(out, 1).cpu(), torch.stack(mag, 1).cpu()
+
+
+@pytest.mark.parametrize("spread", [1.0, 40.0])
+@pytest.mark.parametrize("cached", [False, True])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "x".join(map(str, c)))
+def test_long_key_ranges(ctx, case, cached, spread):
+    n, m, kv_heads, group, block = case
+    q = normal(80, n, kv_heads * group, 128, spread=spread).cuda()
+    k, v = normal(81, m, kv_heads, 128).cuda(), normal(82, m, kv_heads, 128).cuda()
+    if cached:
+        cache = ctx.qcache(1, kv_heads, 128, m + 100)
+        cache.data.fill_(255)
+        ctx.qcache_append(cache, k, v, ints([0]))
+        ctx.qcache_read(cache, k, v, ints([0]))
+        got = ctx.qcache_attention(cache, q, ints([m]), ints([0, n]), causal_block=block)
+    else:
+        got = ctx.packed_attention(q, k, v, ints([0, n]), ints([0, m]), causal_block=block)
+    R.assert_attention(got, *long_reference(q, k, v, block), str(case))
+
+
+def test_even_shares_with_fewer_rows_and_keys_than_planned(ctx):
+    """Offsets and lengths on the device that name less than the tensors hold."""
+    q, k, v = (normal(83 + i, n, 9, 128).cuda() for i, n in enumerate((4200, 8300, 8300)))
+    for nq, nk in ((3000, 8300), (4200, 900), (130, 65), (4200, 0)):
+        out = torch.full_like(q, 9.0)
+        ctx.packed_attention(q, k, v, ints([0, nq]), ints([0, nk]), out=out)
+        assert bool((out[nq:] == 9.0).all())
+        if nk:
+            R.assert_attention(out[:nq], *long_reference(q[:nq], k[:nk], v[:nk], 0), f"{nq} {nk}")
+        else:
+            assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_sequences_in_any_order(ctx, d):
+    """More sequences than are ranked, and fewer, with lengths in no order."""
+    for n_seqs in (20, 90):
+        rng = np.random.default_rng(n_seqs)
+        nq, nk = rng.integers(0, 200, n_seqs).tolist(), rng.integers(0, 300, n_seqs).tolist()
+        packed_case(ctx, (nq, nk, 2, 2, d, 1), seed=90)
+
+
 @pytest.mark.parametrize("spread", [1e-3, 40.0, 1000.0])
 @pytest.mark.parametrize("d", [64, 128])
 def test_packed_attention_logit_range(ctx, spread, d):
