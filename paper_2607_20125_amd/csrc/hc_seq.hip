@@ -11,7 +11,10 @@ using namespace dev;
 // sequence on 4 waves of 32, over the key tiles of its range, 64 keys each.  Tiles go
 // global -> registers -> LDS: the loads of tile t + 1 are issued before the products of
 // tile t, and are converted (4-bit codes) and transposed (V) on their way into the
-// other LDS buffer.  Online softmax with lazy rescaling; layouts as in hc_device.h.
+// other LDS buffer.  Online softmax with lazy rescaling; layouts as in hc_device.h.  Two work groups
+// share a CU, two waves a SIMD, and hide each other's loads and barriers.  (With S(t+1) computed beside
+// the softmax of tile t, as the dense kernels do, 128-dim heads need more than the 256 registers
+// and 64-dim heads gain nothing.)
 // ---------------------------------------------------------------------------
 constexpr int kWaves = kSeqRows / 32;
 
@@ -51,7 +54,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
 
   // --- tiles ---------------------------------------------------------------------
   // K: chunk c (8 dims) of key r goes to LDS row kperm(r), position kswz.  V: 8 keys of
-  // one dim are 16 bytes ([group of 8 keys][d][8]).
+  // one dim are 16 bytes ([group of 8 keys][d][8]); dim d of a group is kept at d ^ (d / 16 % 4), so that
+  // 16 lanes that write 4 dims each reach all banks with each of them.
   constexpr int KI = QUANT ? 1 : TILE / 8 / NT;      // K loads of a thread
   u32x4 kr[KI], vr[QUANT ? 1 : 4];
   uint32_t ks = 0, vs[2] = {0, 0};
@@ -106,6 +110,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
   // dims 2 i, 2 i + 1 of tokens 2 j (x) and 2 j + 1 (y) become words of two tokens
   auto low2 = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); };
   auto high2 = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); };
+  auto put_v_dim = [&](int b, int e, u32x4 w) {
+    const int dim = v_dim + e;
+    *reinterpret_cast<u32x4 *>(&sV[b][(v_grp * D + (dim ^ (dim >> 4 & 3))) * 8]) = w;
+  };
   auto put = [&](int t) {
     const int b = t & 1;
     if constexpr (QUANT) {
@@ -141,7 +149,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
         two(2, vr[0][2], scale_of<0>(s1), scale_of<1>(s1));
         two(3, vr[0][3], scale_of<2>(s1), scale_of<3>(s1));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4 *>(&sV[b][(v_grp * D + v_dim + e) * 8]) = d[e];
+        for (int e = 0; e < 4; ++e) put_v_dim(b, e, d[e]);
       }
     } else {
 #pragma unroll
@@ -159,7 +167,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
           d[3][j] = high2(vr[j][1], vr[j][3]);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4 *>(&sV[b][(v_grp * D + v_dim + e) * 8]) = d[e];
+        for (int e = 0; e < 4; ++e) put_v_dim(b, e, d[e]);
       }
     }
   };
@@ -225,7 +233,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int db = 0; db < NDB; ++db) {
-          const bf16x8 vf = *reinterpret_cast<const bf16x8 *>(&sV[b][((4 * kb + 2 * h + g) * D + 32 * db + n) * 8]);
+          const int dim = 32 * db + n;
+          const bf16x8 vf =
+              *reinterpret_cast<const bf16x8 *>(&sV[b][((4 * kb + 2 * h + g) * D + (dim ^ (dim >> 4 & 3))) * 8]);
           acc[db] = mfma32(vf, pf[kb][h], acc[db]);
         }
     if (t + 1 < t1) {
