@@ -15,10 +15,11 @@ __device__ __forceinline__ uint32_t values2(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, B));
 }
 
-// Byte B of a word of scale codes as its power of two.
+// Byte B of a word of scale codes as its power of two, for values2: the conversion takes the exponent
+// field alone, so the neighbouring codes may stand in the other bits.
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t codes) {
-  return __uint_as_float((codes >> (8 * B) & 0xffu) << 23);
+  return __uint_as_float(B == 3 ? codes >> 1 : codes << (23 - 8 * B));
 }
 
 // One unit of work: rows row0 .. of a sequence (row r is query r / group).

@@ -12,14 +12,15 @@ using namespace dev;
 // global -> registers -> LDS: the loads of tile t + 1 are issued before the products of
 // tile t, and are converted (4-bit codes) and transposed (V) on their way into the
 // other LDS buffer.  Online softmax with lazy rescaling; layouts as in hc_device.h.  Two work groups
-// share a CU, two waves a SIMD, and hide each other's loads and barriers.  (With S(t+1) computed beside
+// (three with 64-dim heads: 5% faster where they fill the card) share a CU, a wave each on every SIMD, and hide each
+// other's loads and barriers.  (With S(t+1) computed beside
 // the softmax of tile t, as the dense kernels do, 128-dim heads need more than the 256 registers
 // and 64-dim heads gain nothing.)
 // ---------------------------------------------------------------------------
 constexpr int kWaves = kSeqRows / 32;
 
 template <int D, bool QUANT>
-__global__ __launch_bounds__(64 * kWaves, 2) void seq_attn_kernel(SeqArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(SeqArgs a) {
   constexpr int KT = kSeqKeys, NKK = D / 16, NDB = D / 32, TILE = KT * D;
   constexpr int NT = 64 * kWaves;
   __shared__ __attribute__((aligned(1024))) uint16_t sK[2][TILE];

@@ -172,12 +172,15 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   const uint8_t *cbase = nullptr;
   u32x4 kraw[2], vraw[2];
   uint32_t ksc[2], vsc[2][2];
-  uint32_t kw_at = 0, vw_at = 0;
+  uint32_t kw_at[4] = {}, vw_at[4] = {};     // for word m % 4 of K, token % 4 of V
   if constexpr (QUANT) {
     cbase = a.cache + ((int64_t)u.seq * a.kv_heads + head) * a.cache_head + (int64_t)t0 * qtile_bytes(D);
     const int key = tid / 4, r = (key & ~31) | kperm(key & 31);
-    kw_at = (uint32_t)(uintptr_t)(lvoid)&sK[0][0] + (uint32_t)(r * 256 + kswz<D>(r, 4 * (tid % 4)) * 16);
-    vw_at = (uint32_t)(uintptr_t)(lvoid)&sV[0][0] + (uint32_t)((tid / 32) * 8 * 256 + (tid % 32) * 8);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      kw_at[m] = (uint32_t)(uintptr_t)(lvoid)&sK[0][0] + (uint32_t)(r * 256 + kswz<D>(r, 4 * (tid % 4) + m) * 16);
+      vw_at[m] = (uint32_t)(uintptr_t)(lvoid)&sV[0][0] + (uint32_t)((tid / 32) * 8 * 256 + (((tid % 32) * 8) ^ (64 * m)));
+    }
   }
   auto load_k = [&](int t) {
     const uint8_t *tp = cbase + (int64_t)t * qtile_bytes(D);
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     const int e = i / 4, m = i % 4;
     const uint32_t w = kraw[e][m];
     const float scale = __uint_as_float(ksc[e] << 23);
-    *(lds16w)(uintptr_t)((kw_at ^ (uint32_t)(m * 16)) + slot + (uint32_t)(e * 32 * 256)) =
+    *(lds16w)(uintptr_t)(kw_at[m] + slot + (uint32_t)(e * 32 * 256)) =
         u32x4{values2<0>(w, scale), values2<1>(w, scale), values2<2>(w, scale), values2<3>(w, scale)};
   };
   auto put_v = [&](uint32_t slot, int i) {
@@ -225,8 +228,8 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     const uint32_t w = vraw[e][m], s = vsc[e][m / 2];
     const float sx = m % 2 ? scale_of<2>(s) : scale_of<0>(s), sy = m % 2 ? scale_of<3>(s) : scale_of<1>(s);
     const uint32_t at = slot + (uint32_t)((e * 32 + 2 * m) * 256);
-    *(lds8w)(uintptr_t)((vw_at ^ (uint32_t)((2 * m % 4) * 64)) + at) = u32x2{values2<0>(w, sx), values2<1>(w, sx)};
-    *(lds8w)(uintptr_t)((vw_at ^ (uint32_t)((2 * m % 4 + 1) * 64)) + at + 256) =
+    *(lds8w)(uintptr_t)(vw_at[2 * m % 4] + at) = u32x2{values2<0>(w, sx), values2<1>(w, sx)};
+    *(lds8w)(uintptr_t)(vw_at[2 * m % 4 + 1] + at + 256) =
         u32x2{values2<2>(w, sy), values2<3>(w, sy)};
   };
   auto k_slot = [&](int t) { return (uint32_t)((t % RK) * TILE * 2); };
