@@ -362,6 +362,72 @@ def test_packed_bad_values_stay_in_their_sequence(ctx):
     assert not torch.isfinite(got[50:90]).any()
 
 
+def test_packed_bad_values_stay_in_their_sequence_over_long_ranges(ctx):
+    """The same where the written-out steps run, with sequences that share neither rows nor tiles."""
+    n = 2100
+    q, k, v = (normal(49 + i, 2 * n, 2, 128).cuda() for i in range(3))
+    k[n:], v[n:] = math.nan, math.nan
+    got = ctx.packed_attention(q, k, v, ints([0, n, 2 * n]), causal_block=0)
+    R.assert_attention(got[:n], *long_reference(q[:n], k[:n], v[:n], 0))
+    assert bool(torch.isnan(got[n:]).all())
+
+
+def test_two_graphs_with_workspaces_of_their_own(ctx):
+    """Two captured calls that need room for partial results, replayed at the same time on two streams."""
+    n, m = 5, 6000
+    sides = []
+    for s in range(2):
+        q, k, v = normal(52 + s, n, 4, 128).cuda(), normal(54 + s, m, 2, 128).cuda(), normal(56 + s, m, 2, 128).cuda()
+        cu = (ints([0, n]), ints([0, m]))
+        out = torch.zeros_like(q)
+        work = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+        call = lambda q=q, k=k, v=v, cu=cu, out=out, work=work: ctx.packed_attention(q, k, v, *cu, out=out, causal_block=1, workspace=work)  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        want = out.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        sides.append((graph, out, want, torch.cuda.Stream(), call))     # (the call holds its tensors)
+    for _ in range(5):
+        for _, out, _, _, _ in sides:
+            out.zero_()
+        torch.cuda.synchronize()
+        for graph, _, _, stream, _ in sides:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, out, want, _, _ in sides:
+            assert torch.equal(out, want)
+
+
+def test_refusals_through_the_binding(ctx, hc):
+    q = normal(58, 8, 4, 64).cuda()
+    cu = ints([0, 8])
+    with pytest.raises(ValueError, match="bfloat16"):
+        ctx.packed_attention(q.float(), q, q, cu)
+    with pytest.raises(hc.HeadCastError, match="multiple of n_kv_heads"):
+        ctx.packed_attention(q, q[:, :3], q[:, :3], cu)
+    with pytest.raises(hc.HeadCastError, match="strides"):
+        odd = torch.zeros(8, 4, 68, dtype=BF, device="cuda")[..., :64]
+        ctx.packed_attention(odd, q, q, cu)
+    with pytest.raises(hc.HeadCastError, match="rows overlap"):
+        ctx.packed_attention(q, q, q, cu, out=torch.zeros(1, 4, 64, dtype=BF, device="cuda").expand(8, 4, 64))
+    with pytest.raises(hc.HeadCastError, match="workspace"):
+        k = normal(59, 6000, 1, 64).cuda()
+        ctx.packed_attention(q[:2, :1], k, k, ints([0, 2]), ints([0, 6000]),
+                             workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError, match="int32"):
+        ctx.packed_attention(q, q, q, cu.long())
+    with pytest.raises(hc.HeadCastError, match="axis_dims"):
+        ctx.rotate(q, axis_dims=(24, 20, 10))
+    cache = ctx.qcache(1, 4, 64, 10)
+    with pytest.raises(ValueError, match="start"):
+        ctx.qcache_append(cache, q, q, ints([0, 0]))
+    with pytest.raises(ValueError, match="expected shape"):
+        ctx.qcache_append(cache, q[:, :2], q, ints([0]))
+
+
 # --- attention over the 4-bit cache --------------------------------------------------------------
 
 CACHED = [
