@@ -282,7 +282,8 @@ hc_status hc_memory_bytes(const hc_ctx *ctx, int64_t *bytes);
  * partial results takes it from the caller, and two graphs (or two calls at once)
  * need a workspace each.  The calling thread's current device is left as it was.
  * Pointers are 16-byte aligned unless said otherwise, strides are in elements and
- * multiples of 8 (neighbouring dims of a head are always 1 apart).  Lengths and
+ * multiples of 8 (neighbouring dims of a head are always 1 apart; the stride of an axis of
+ * length 1 is not looked at).  Lengths and
  * offsets in device memory are read when the call runs: they cannot be checked
  * by the host, and values out of range are clamped, so that nothing outside the
  * given tensors is read or written.

@@ -28,33 +28,34 @@ struct OnDevice {
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Strides of a tensor of 16-byte vectors.
-bool good_strides(int64_t token, int64_t head) {
-  return token >= 0 && head >= 0 && token % 8 == 0 && head % 8 == 0;
-}
-
 // Work groups of a launch dimension, of 256 threads at most: the runtime counts threads in 32 bits.
 bool good_grid(int64_t groups) { return groups <= (int64_t)UINT32_MAX / 256; }
 
-hc_status check_tensor(hc_ctx *c, const char *name, const void *p, int64_t token, int64_t head) {
-  if (!p || !aligned16(p)) return fail(c, HC_E_INVAL, "%s must be a 16-byte aligned device pointer", name);
-  if (!good_strides(token, head))
-    return fail(c, HC_E_INVAL, "%s: strides must be multiples of 8 and not negative", name);
+// A tensor of rows that are moved as 16-byte vectors.  (The stride of an axis of length 1 says nothing.)
+struct Rows {
+  const char *name;
+  const void *p;
+  int64_t token, head, n_tokens, n_heads;
+};
+hc_status check_tensor(hc_ctx *c, const Rows &t) {
+  if (!t.p || !aligned16(t.p)) return fail(c, HC_E_INVAL, "%s must be a 16-byte aligned device pointer", t.name);
+  auto good = [](int64_t stride, int64_t n) { return n <= 1 || (stride >= 0 && stride % 8 == 0); };
+  if (!good(t.token, t.n_tokens) || !good(t.head, t.n_heads))
+    return fail(c, HC_E_INVAL, "%s: strides must be multiples of 8 and not negative", t.name);
   return HC_OK;
 }
 
 // A tensor that a call writes: besides, no two of its rows of `dim` values overlap.
-hc_status check_output(hc_ctx *c, const char *name, const void *p, int64_t token, int64_t head,
-                       int64_t n_tokens, int64_t n_heads, int dim) {
-  hc_status st = check_tensor(c, name, p, token, head);
+hc_status check_output(hc_ctx *c, const Rows &t, int dim) {
+  hc_status st = check_tensor(c, t);
   if (st != HC_OK) return st;
   int64_t end = dim;                           // behind the rows along the shorter stride
-  const bool heads_first = n_tokens == 1 || (n_heads > 1 && head <= token);
+  const bool heads_first = t.n_tokens <= 1 || (t.n_heads > 1 && t.head <= t.token);
   for (int i = 0; i < 2; ++i) {
     const bool heads = heads_first == (i == 0);
-    const int64_t n = heads ? n_heads : n_tokens, stride = heads ? head : token;
+    const int64_t n = heads ? t.n_heads : t.n_tokens, stride = heads ? t.head : t.token;
     if (n <= 1) continue;
-    if (stride < end) return fail(c, HC_E_INVAL, "%s: rows overlap", name);
+    if (stride < end) return fail(c, HC_E_INVAL, "%s: rows overlap", t.name);
     end += stride > (INT64_MAX - end) / n ? INT64_MAX - end : (n - 1) * stride;
   }
   return HC_OK;
@@ -212,11 +213,9 @@ hc_status cache_rows(hc_ctx *c, const hc_qcache *k, const hc_qcache_rows *r, boo
   if (r->n_tokens < 0) return fail(c, HC_E_INVAL, "n_tokens must not be negative");
   if ((st = check_parts(c, "cu_seqlens", r->cu_seqlens, r->n_tokens, k->n_seqs)) != HC_OK) return st;
   if (r->n_tokens == 0) return HC_OK;
-  struct { const char *name; const void *p; int64_t token, head; } both[] = {
-      {"k", r->k, r->k_token, r->k_head}, {"v", r->v, r->v_token, r->v_head}};
-  for (const auto &t : both) {
-    st = writes ? check_output(c, t.name, t.p, t.token, t.head, r->n_tokens, k->n_heads, k->head_dim)
-                : check_tensor(c, t.name, t.p, t.token, t.head);
+  for (const Rows &t : {Rows{"k", r->k, r->k_token, r->k_head, r->n_tokens, k->n_heads},
+                        Rows{"v", r->v, r->v_token, r->v_head, r->n_tokens, k->n_heads}}) {
+    st = writes ? check_output(c, t, k->head_dim) : check_tensor(c, t);
     if (st != HC_OK) return st;
   }
   if (!r->start || !aligned4(r->start)) return fail(c, HC_E_INVAL, "start must be a 4-byte aligned device pointer");
@@ -311,11 +310,12 @@ hc_status hc_rotate(hc_ctx *c, const hc_rotate_args *p, const hc_rotate_tensor *
     if (t[i].n_heads < 1) return fail(c, HC_E_INVAL, "tensor %d: n_heads must be at least 1", i);
     heads += t[i].n_heads;
     if (p->n_tokens == 0) continue;
-    hc_status st = check_tensor(c, "x", t[i].x, t[i].x_token, t[i].x_head);
+    hc_status st = check_tensor(c, {"x", t[i].x, t[i].x_token, t[i].x_head, p->n_tokens, t[i].n_heads});
     if (st == HC_OK)
-      st = check_output(c, "out", t[i].out, t[i].out_token, t[i].out_head, p->n_tokens, t[i].n_heads, p->head_dim);
+      st = check_output(c, {"out", t[i].out, t[i].out_token, t[i].out_head, p->n_tokens, t[i].n_heads}, p->head_dim);
     if (st != HC_OK) return st;
-    if (t[i].x == t[i].out && (p->x_type != p->out_type || t[i].x_token != t[i].out_token || t[i].x_head != t[i].out_head))
+    if (t[i].x == t[i].out && (p->x_type != p->out_type || (p->n_tokens > 1 && t[i].x_token != t[i].out_token) ||
+                               (t[i].n_heads > 1 && t[i].x_head != t[i].out_head)))
       return fail(c, HC_E_INVAL, "tensor %d: in place needs the same type and strides", i);
     a.t[i] = t[i];
   }
@@ -359,13 +359,13 @@ hc_status hc_packed_attention(hc_ctx *c, const hc_packed_args *p, hc_stream stre
   hc_status st = packed_plan(c, p, a);
   if (st != HC_OK) return st;
   if (p->n_tokens == 0) return HC_OK;
-  if ((st = check_tensor(c, "q", p->q, p->q_token, p->q_head)) != HC_OK) return st;
-  if ((st = check_output(c, "out", p->out, p->out_token, p->out_head, p->n_tokens, p->n_heads, p->head_dim)) != HC_OK)
-    return st;
-  if (p->n_keys > 0) {
-    if ((st = check_tensor(c, "k", p->k, p->k_token, p->k_head)) != HC_OK) return st;
-    if ((st = check_tensor(c, "v", p->v, p->v_token, p->v_head)) != HC_OK) return st;
-  }
+  st = check_tensor(c, {"q", p->q, p->q_token, p->q_head, p->n_tokens, p->n_heads});
+  if (st == HC_OK) st = check_output(c, {"out", p->out, p->out_token, p->out_head, p->n_tokens, p->n_heads}, p->head_dim);
+  if (st == HC_OK && p->n_keys > 0)
+    st = check_tensor(c, {"k", p->k, p->k_token, p->k_head, p->n_keys, p->n_kv_heads});
+  if (st == HC_OK && p->n_keys > 0)
+    st = check_tensor(c, {"v", p->v, p->v_token, p->v_head, p->n_keys, p->n_kv_heads});
+  if (st != HC_OK) return st;
   if ((st = check_workspace(c, p->workspace, p->workspace_bytes, part_bytes(a, p->head_dim, kSeqRows))) != HC_OK)
     return st;
   if (a.n_split > 1) use_workspace(a, p->workspace);
@@ -409,9 +409,9 @@ hc_status hc_qcache_attention(hc_ctx *c, const hc_qcache *k, const hc_qcache_att
   if (st == HC_OK) st = cached_plan(c, k, p, a, few_rows);
   if (st != HC_OK) return st;
   if (p->n_tokens == 0) return HC_OK;
-  if ((st = check_tensor(c, "q", p->q, p->q_token, p->q_head)) != HC_OK) return st;
-  if ((st = check_output(c, "out", p->out, p->out_token, p->out_head, p->n_tokens, p->n_heads, k->head_dim)) != HC_OK)
-    return st;
+  st = check_tensor(c, {"q", p->q, p->q_token, p->q_head, p->n_tokens, p->n_heads});
+  if (st == HC_OK) st = check_output(c, {"out", p->out, p->out_token, p->out_head, p->n_tokens, p->n_heads}, k->head_dim);
+  if (st != HC_OK) return st;
   if (!p->kv_len || !aligned4(p->kv_len)) return fail(c, HC_E_INVAL, "kv_len must be a 4-byte aligned device pointer");
   if ((st = check_workspace(c, p->workspace, p->workspace_bytes,
                             part_bytes(a, k->head_dim, few_rows ? kDecodeRows : kSeqRows))) != HC_OK)

@@ -8,11 +8,11 @@ raises on import instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 import struct
 
 import numpy as np
+import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libheadcast.so")
 
@@ -119,19 +119,13 @@ def _load() -> ctypes.CDLL:
         "hc_profile_read": (ctypes.c_int, [P, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                                            ctypes.POINTER(I64)]),
         "hc_rotate": (ctypes.c_int, [P, P, P, ctypes.c_int, P]),
-        "hc_packed_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs),
-                                               ctypes.POINTER(I64)]),
-        "hc_packed_attention": (ctypes.c_int, [P, ctypes.POINTER(HCPackedArgs), P]),
+        "hc_packed_workspace": (ctypes.c_int, [P, P, ctypes.POINTER(I64)]),
+        "hc_packed_attention": (ctypes.c_int, [P, P, P]),
         "hc_qcache_bytes": (ctypes.c_int, [ctypes.POINTER(HCQCache), ctypes.POINTER(I64)]),
-        "hc_qcache_append": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
-                                            ctypes.POINTER(HCQCacheRows), P]),
-        "hc_qcache_read": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
-                                          ctypes.POINTER(HCQCacheRows), P]),
-        "hc_qcache_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
-                                               ctypes.POINTER(HCQCacheAttentionArgs),
-                                               ctypes.POINTER(I64)]),
-        "hc_qcache_attention": (ctypes.c_int, [P, ctypes.POINTER(HCQCache),
-                                               ctypes.POINTER(HCQCacheAttentionArgs), P]),
+        "hc_qcache_append": (ctypes.c_int, [P, ctypes.POINTER(HCQCache), P, P]),
+        "hc_qcache_read": (ctypes.c_int, [P, ctypes.POINTER(HCQCache), P, P]),
+        "hc_qcache_workspace": (ctypes.c_int, [P, ctypes.POINTER(HCQCache), P, ctypes.POINTER(I64)]),
+        "hc_qcache_attention": (ctypes.c_int, [P, ctypes.POINTER(HCQCache), P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -185,40 +179,24 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-@functools.lru_cache(maxsize=None)
-def _torch():
-    import torch
-    return torch
+# The argument structures as native bytes: packing them costs a call a fifth of what filling ctypes
+# structures does, which counts where the kernel takes 4 us.
+def _packer(layout, *kinds):
+    assert struct.calcsize(layout) == sum(ctypes.sizeof(k) for k in kinds), layout
+    return struct.Struct(layout).pack
 
 
-@functools.lru_cache(maxsize=None)
-def _rotate_types():
-    return {_torch().bfloat16: BF16, _torch().float32: F32}
-
-
-@functools.lru_cache(maxsize=None)
-def _bf16():
-    return (_torch().bfloat16,)
-
-
-# The two structures of a rotation as native bytes: packing them costs a call a fifth of what filling
-# ctypes structures does, which counts where the kernel takes 4 us.
-_PACK_ROTATE = struct.Struct("@12i3idP").pack
-_PACK_TENSOR = {1: struct.Struct("@2P4qi4x").pack, 2: struct.Struct("@2P4qi4x2P4qi4x").pack}
-assert struct.calcsize("@12i3idP") == ctypes.sizeof(HCRotateArgs)
-assert struct.calcsize("@2P4qi4x") == ctypes.sizeof(HCRotateTensor)
-
-
-@functools.lru_cache(maxsize=None)
-def _raw_stream_of():
-    """torch's way to its current stream of a device as a hipStream_t (the short one if it is there)."""
-    torch = _torch()
-    return (getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            or (lambda device: torch.cuda.current_stream(device).cuda_stream))
-
-
-def _raw_stream(device):
-    return _raw_stream_of()(device)
+_PACK_ROTATE = _packer("@15idP", HCRotateArgs)
+_PACK_TENSOR = {1: _packer("@2P4qi4x", HCRotateTensor),
+                2: _packer("@2P4qi4x2P4qi4x", HCRotateTensor, HCRotateTensor)}
+_PACK_PACKED = _packer("@4P8q7if3Pq", HCPackedArgs)
+_PACK_ROWS = _packer("@2P4qi4x2P", HCQCacheRows)
+_PACK_CACHED = _packer("@2P4q4if4x3Pq", HCQCacheAttentionArgs)
+_BF16 = (torch.bfloat16,)
+_ROTATE_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+# torch's current stream of a device as a hipStream_t: the short way where torch has it
+_raw_stream = (getattr(torch._C, "_cuda_getCurrentRawStream", None)
+               or (lambda device: torch.cuda.current_stream(device).cuda_stream))
 
 
 class QCache:
@@ -226,7 +204,6 @@ class QCache:
     sequences of up to `capacity` tokens.  `Context.qcache` makes one."""
 
     def __init__(self, n_seqs: int, n_heads: int, head_dim: int, capacity: int, device):
-        import torch
         for name, value in (("n_seqs", n_seqs), ("n_heads", n_heads), ("capacity", capacity)):
             if not 1 <= value < 1 << 31:
                 raise ValueError(f"{name} must be at least 1 and below 2^31, got {value}")
@@ -247,7 +224,7 @@ class Context:
     def __init__(self, cfg: HCConfig, device: int = 0):
         self.cfg = cfg
         self.device = device
-        self._torch_device = f"cuda:{device}"
+        self._need = ctypes.c_int64()
         self._h = ctypes.c_void_p()
         st = lib.hc_create(ctypes.byref(cfg), device, ctypes.byref(self._h))
         if st != HC_OK:
@@ -369,38 +346,35 @@ class Context:
 
     def _rows(self, name, t, dtypes, shape=None):
         """Pointer and strides of a [tokens][heads][head_dim] tensor on this context's device."""
-        s, st = t.shape, t.stride()
+        st = t.stride()
+        if (len(st) == 3 and st[2] == 1 and t.dtype in dtypes and t.get_device() == self.device
+                and (shape is None or t.shape == shape)):
+            return t.data_ptr(), st[0], st[1]
         if t.dtype not in dtypes or t.get_device() != self.device:
             raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))} on cuda:{self.device}, "
                              f"got {t.dtype} on {t.device}")
-        if len(s) != 3 or (shape is not None and s != shape):
+        if len(st) != 3 or (shape is not None and t.shape != shape):
             raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[tokens][heads][head_dim]'}, "
-                             f"got {tuple(s)}")
-        if st[2] != 1 and s[2] > 1 and s[0] and s[1]:
+                             f"got {tuple(t.shape)}")
+        if t.numel():
             raise ValueError(f"{name}: neighbouring dims of a head must be adjacent in memory")
-        # (the stride of an axis of length 1 says nothing and may be anything)
-        return t.data_ptr(), st[0] if s[0] > 1 else 0, st[1] if s[1] > 1 else 0
+        return t.data_ptr(), 0, 0
 
     def _ints(self, name, t, shape):
         if t is None:
-            return None
-        if t.dtype is not _torch().int32 or t.get_device() != self.device or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on "
-                             f"cuda:{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+            return 0
+        if (t.dtype is torch.int32 and t.get_device() == self.device and t.shape == shape and t.is_contiguous()):
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {tuple(shape)} on "
+                         f"cuda:{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
-    def _work(self, args, nbytes, workspace):
-        """Puts a workspace of `nbytes` bytes into args: the caller's, or one that lives until
-        the tensor returned here is dropped (torch keeps its memory from other streams' work)."""
-        if nbytes == 0:
-            return None
+    def _work(self, workspace):
+        """The caller's workspace, or one of the needed size, which torch keeps from other streams' work
+        until it is dropped behind the call."""
         if workspace is None:
-            torch = _torch()
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=self._torch_device)
-        elif not workspace.is_cuda or workspace.device.index != self.device or not workspace.is_contiguous():
+            return torch.empty(self._need.value, dtype=torch.uint8, device=torch.device("cuda", self.device))
+        if workspace.get_device() != self.device or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected a contiguous tensor on cuda:{self.device}")
-        args.workspace = workspace.data_ptr()
-        args.workspace_bytes = workspace.numel() * workspace.element_size()
         return workspace
 
     def rotate(self, x, out=None, *, axis_dims, positions=None, grid=None, frame0=0,
@@ -413,7 +387,7 @@ class Context:
         pair = isinstance(x, (tuple, list))
         xs = x if pair else (x,)
         if out is None:
-            outs = tuple([_torch().empty(t.shape, dtype=t.dtype, device=t.device) for t in xs])
+            outs = tuple([torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs])
         else:
             outs = out if isinstance(out, (tuple, list)) else (out,)
         n_tensors, n_axes = len(xs), len(axis_dims)
@@ -421,7 +395,7 @@ class Context:
             raise ValueError("rotate takes one tensor or a pair, and as many outputs")
         if not 1 <= n_axes <= 4:
             raise ValueError("axis_dims must have one to four entries")
-        types = _rotate_types()
+        types = _ROTATE_TYPES
         n, _, d = xs[0].shape if xs[0].dim() == 3 else (0, 0, -1)
         x_type, out_type = xs[0].dtype, outs[0].dtype
         tensors = []
@@ -435,7 +409,7 @@ class Context:
         gh, gw = (self.cfg.grid_h, self.cfg.grid_w) if grid is None else grid
         args = _PACK_ROTATE(n, d, types[x_type], types[out_type], n_axes, *axis_dims, *(0,) * (4 - n_axes),
                             bool(halves), bool(joint), bool(inverse), gh, gw, frame0, theta,
-                            0 if positions is None else self._ints("positions", positions, (n_axes, n)))
+                            self._ints("positions", positions, (n_axes, n)))
         status = lib.hc_rotate(self._h, args, _PACK_TENSOR[n_tensors](*tensors), n_tensors, _raw_stream(self.device))
         if status:
             self._check(status, "hc_rotate")
@@ -446,30 +420,32 @@ class Context:
         """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
         cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
         None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
-        bf16 = _bf16()
         if out is None:
-            out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if n_seqs is None:
             n_seqs = cu_q.shape[0] - 1 if cu_q is not None else 1
         qs, ks = q.shape, k.shape
-        qp, qt, qh = self._rows("q", q, bf16)
-        kp, kt, kh = self._rows("k", k, bf16)
-        vp, vt, vh = self._rows("v", v, bf16, ks)
-        op, ot, oh = self._rows("out", out, bf16, qs)
-        if ks[2] != qs[2]:
-            raise ValueError(f"k: expected heads of {qs[2]} dims, got {tuple(ks)}")
-        a = HCPackedArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, qs[0], ks[0], n_seqs, qs[1], ks[1], qs[2],
-                         causal_block, softmax_scale, self._ints("cu_q", cu_q, (n_seqs + 1,)),
-                         self._ints("cu_k", cu_k, (n_seqs + 1,)))
-        need = ctypes.c_int64()
-        status = lib.hc_packed_workspace(self._h, a, need)
+        qp, qt, qh = self._rows("q", q, _BF16)
+        kp, kt, kh = self._rows("k", k, _BF16)
+        vp, vt, vh = self._rows("v", v, _BF16, ks)
+        op, ot, oh = self._rows("out", out, _BF16, qs)
+        n, heads, d = qs
+        m, kv_heads, kd = ks
+        if kd != d:
+            raise ValueError(f"k: expected heads of {d} dims, got {tuple(ks)}")
+        args = (qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, n, m, n_seqs, heads, kv_heads, d, causal_block,
+                softmax_scale, self._ints("cu_q", cu_q, (n_seqs + 1,)), self._ints("cu_k", cu_k, (n_seqs + 1,)))
+        packed = _PACK_PACKED(*args, 0, 0)
+        need = self._need
+        status = lib.hc_packed_workspace(self._h, packed, need)
         if status:
             self._check(status, "hc_packed_workspace")
-        held = self._work(a, need.value, workspace)
-        status = lib.hc_packed_attention(self._h, a, _raw_stream(self.device))
+        if need.value:
+            workspace = self._work(workspace)
+            packed = _PACK_PACKED(*args, workspace.data_ptr(), workspace.nbytes)
+        status = lib.hc_packed_attention(self._h, packed, _raw_stream(self.device))
         if status:
             self._check(status, "hc_packed_attention")
-        del held
         return out
 
     def qcache(self, n_seqs: int, n_heads: int, head_dim: int, capacity: int) -> QCache:
@@ -477,12 +453,17 @@ class Context:
         return QCache(n_seqs, n_heads, head_dim, capacity, f"cuda:{self.device}")
 
     def _cache_rows(self, fn, what, cache, k, v, start, cu_seqlens):
-        shape = (k.shape[0], cache.n_heads, cache.head_dim)
-        kp, kt, kh = self._rows("k", k, _bf16(), shape)
-        vp, vt, vh = self._rows("v", v, _bf16(), shape)
-        r = HCQCacheRows(kp, vp, kt, kh, vt, vh, shape[0], self._ints("start", start, (cache.n_seqs,)),
-                         self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
-        status = fn(self._h, cache.desc, r, _raw_stream(self.device))
+        shape = k.shape
+        kp, kt, kh = self._rows("k", k, _BF16)
+        vp, vt, vh = self._rows("v", v, _BF16, shape)
+        n, heads, d = shape
+        if cache.data.get_device() != self.device:
+            raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
+        if heads != cache.n_heads or d != cache.head_dim:
+            raise ValueError(f"k: expected shape [tokens][{cache.n_heads}][{cache.head_dim}], got {tuple(shape)}")
+        rows = _PACK_ROWS(kp, vp, kt, kh, vt, vh, n, self._ints("start", start, (cache.n_seqs,)),
+                          self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
+        status = fn(self._h, cache.desc, rows, _raw_stream(self.device))
         if status:
             self._check(status, what)
 
@@ -499,24 +480,28 @@ class Context:
                          causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
         """hc_qcache_attention: attention of q over the first kv_len[s] (int32 [n_seqs]) slots
         of each sequence of the cache.  Returns `out` (bf16, the shape of q)."""
-        bf16 = _bf16()
         if out is None:
-            out = _torch().empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         qs = q.shape
-        qp, qt, qh = self._rows("q", q, bf16)
-        op, ot, oh = self._rows("out", out, bf16, qs)
-        if qs[2] != cache.head_dim:
+        qp, qt, qh = self._rows("q", q, _BF16)
+        op, ot, oh = self._rows("out", out, _BF16, qs)
+        n, heads, d = qs
+        if cache.data.get_device() != self.device:
+            raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
+        if d != cache.head_dim:
             raise ValueError(f"q: expected heads of {cache.head_dim} dims, got {tuple(qs)}")
-        a = HCQCacheAttentionArgs(qp, op, qt, qh, ot, oh, qs[0], qs[1], causal_block, max_kv, softmax_scale,
-                                  self._ints("kv_len", kv_len, (cache.n_seqs,)),
-                                  self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
-        need = ctypes.c_int64()
-        status = lib.hc_qcache_workspace(self._h, cache.desc, a, need)
+        args = (qp, op, qt, qh, ot, oh, n, heads, causal_block, max_kv, softmax_scale,
+                self._ints("kv_len", kv_len, (cache.n_seqs,)),
+                self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
+        packed = _PACK_CACHED(*args, 0, 0)
+        need = self._need
+        status = lib.hc_qcache_workspace(self._h, cache.desc, packed, need)
         if status:
             self._check(status, "hc_qcache_workspace")
-        held = self._work(a, need.value, workspace)
-        status = lib.hc_qcache_attention(self._h, cache.desc, a, _raw_stream(self.device))
+        if need.value:
+            workspace = self._work(workspace)
+            packed = _PACK_CACHED(*args, workspace.data_ptr(), workspace.nbytes)
+        status = lib.hc_qcache_attention(self._h, cache.desc, packed, _raw_stream(self.device))
         if status:
             self._check(status, "hc_qcache_attention")
-        del held
         return out

@@ -352,6 +352,18 @@ def test_packed_head_major_and_shared_rows(ctx):
     R.assert_attention(out, *R.attention(q.transpose(0, 1), k.transpose(0, 1), v.transpose(0, 1), 1))
 
 
+def test_strides_of_axes_of_length_one(ctx):
+    """One token, one key and one head cut out of larger tensors at any stride."""
+    q = normal(60, 3, 5, 68).cuda().as_strided((1, 1, 64), (3, 5, 1))
+    k = normal(61, 3, 5, 68).cuda().as_strided((1, 1, 64), (7, 1, 1))
+    out = torch.zeros(1, 1, 64, dtype=BF, device="cuda").as_strided((1, 1, 64), (1, 1, 1))
+    ctx.packed_attention(q, k, k, out=out, causal_block=1)
+    assert torch.equal(out, k)
+    turned = ctx.rotate(q, axis_dims=(24, 20, 20), grid=(1, 1), frame0=5)
+    ref = R.rotate(q.cpu(), torch.tensor([[5], [0], [0]]), (24, 20, 20))
+    assert bool(((turned.cpu().double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-5).all())
+
+
 def test_packed_bad_values_stay_in_their_sequence(ctx):
     nq = [50, 40, 60]
     q, k, v = normal(46, 150, 2, 128), normal(47, 150, 2, 128), normal(48, 150, 2, 128)
