@@ -11,7 +11,8 @@ using namespace dev;
 // share a scale.  Consecutive lanes take 8 tokens, then the 32-dim groups of a head: the
 // codes of a V group of 8 tokens are interleaved by token.
 //
-// Bound by memory: append reads 2 bytes a value and writes 17/32, read the reverse.
+// Bound by memory: append reads 2 bytes a value and writes 17/32, read the reverse (84 MB each
+// for a 720P block of 12 heads: 20.9 us and 23.4 us, 4.0 and 3.6 TB/s).
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 

@@ -18,6 +18,8 @@ using namespace dev;
 // step in 64 bits, less the whole turns, then the hardware's sine and cosine of a
 // fraction of a turn (8.5e-8 off at most over [-0.6, 0.6], measured).  No table: at
 // 128 dims a token costs 64 sines and cosines against 3 KB and more of queries and keys.
+// Measured: queries and keys of a 720P block (12 + 12 heads, 133 MB in and out) 21.6 to 27 us, 4.9 to
+// 6.2 TB/s (more where the last outputs are still cached); 4099 tokens of 20 heads in float32 (84 MB) 17.5 us.
 // ---------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kInFlight = 4;      // heads that a thread loads before it stores the first
