@@ -180,7 +180,9 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
   if (rows > INT32_MAX - kSeqRows || !good_grid(tiles * a.kv_heads))
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
-  choose_split(a, p->n_keys / p->n_seqs, 512, 8, kSeqMaxSplit);
+  // (the host knows how many keys the sequences have together, not how they are shared: the longest
+  // of several, which ends last, is taken for twice the average)
+  choose_split(a, (int64_t)p->n_keys / p->n_seqs * (p->cu_q && p->n_seqs > 1 ? 2 : 1), 512, 8, kSeqMaxSplit);
   // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
   a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24 &&
            wide_rows(a, p->n_keys / p->n_seqs);

@@ -53,9 +53,9 @@ __device__ __forceinline__ void lds_dma16_offsets(const uint16_t *base, const ui
       "s_mov_b32 m0, %6\n\t"
       "s_nop 4\n\t"
       "global_load_lds_dwordx4 %1, %5\n\t"
-      "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-      "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-      "global_load_lds_dwordx4 %4, %5 offset:3072\n\t"
+      "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+      "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
+      "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
       : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base), "s"(lds)
@@ -69,9 +69,9 @@ __device__ __forceinline__ void lds_dma16_bases(const uint16_t *base, int64_t st
       "s_mov_b32 m0, %6\n\t"
       "s_nop 4\n\t"
       "global_load_lds_dwordx4 %1, %2\n\t"
-      "global_load_lds_dwordx4 %1, %3 offset:1024\n\t"
-      "global_load_lds_dwordx4 %1, %4 offset:2048\n\t"
-      "global_load_lds_dwordx4 %1, %5 offset:3072\n\t"
+      "global_load_lds_dwordx4 %1, %3 offset:0x400\n\t"
+      "global_load_lds_dwordx4 %1, %4 offset:0x800\n\t"
+      "global_load_lds_dwordx4 %1, %5 offset:0xc00\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
       : "v"(a), "s"(base), "s"(b1), "s"(b2), "s"(b3), "s"(lds)
