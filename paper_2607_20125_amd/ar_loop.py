@@ -36,7 +36,7 @@ class LoopResult:
 
 
 def run(ctx: hc.Context, n_blocks: int, block_data, out, steps=TIMESTEPS, classify=True,
-        on_step=None, tables_at_fill=None) -> LoopResult:
+        on_step=None, tables_at_fill=None, axis_dims=None) -> LoopResult:
     """Runs `n_blocks` blocks of `len(steps)` denoising steps over every layer.
 
     block_data(layer, block, step) -> (q, k, v): bf16 device tensors [H][L][d]
@@ -44,6 +44,9 @@ def run(ctx: hc.Context, n_blocks: int, block_data, out, steps=TIMESTEPS, classi
         step of a block wrote.
     out: float32 device tensor [H][L][d], reused as the output of every call.
     on_step(layer, block, step, types, q): called after each attention (tests).
+    axis_dims: block_data's q and k carry no positions yet: they are rotated by the
+        (frame, row, column) of their tokens, `hc_rotate` with these dims per axis,
+        before anything else sees them.
     Classification fires at the first step of block W-1 when `classify`;
     otherwise the head table stays all Global (the full-window schedule), or,
     when `tables_at_fill` (per layer) is given, those tables are installed at
@@ -69,6 +72,11 @@ def run(ctx: hc.Context, n_blocks: int, block_data, out, steps=TIMESTEPS, classi
         for si, t in enumerate(steps):
             for layer in range(NL):
                 q, k, v = block_data(layer, b, si)
+                if axis_dims is not None:
+                    turned = torch.empty_like(q), torch.empty_like(k)
+                    ctx.rotate([t.transpose(0, 1) for t in (q, k)], [t.transpose(0, 1) for t in turned],
+                               axis_dims=axis_dims, frame0=b * cfg.frames_per_block)
+                    q, k = turned
                 if tables_at_fill is not None and b == W - 1 and si == 0:
                     kw = torch.cat([held_k[layer][j] for j in range(b)] + [k], dim=1)
                     vw = torch.cat([held_v[layer][j] for j in range(b)] + [v], dim=1)

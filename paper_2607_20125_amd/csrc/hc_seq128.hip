@@ -185,9 +185,12 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       kw_at[m] = (uint32_t)(uintptr_t)(lvoid)&sK[0][0] + (uint32_t)(r * 256 + kswz<D>(r, 4 * (tid % 4) + m) * 16);
-      vw_at[m] = (uint32_t)(uintptr_t)(lvoid)&sV[0][0] + (uint32_t)((tid / 32) * 8 * 256 + (((tid % 32) * 8) ^ (64 * m)));
+      vw_at[m] = (uint32_t)(uintptr_t)(lvoid)&sV[0][0] + (uint32_t)((tid / 32) * 8 * 256 + ((((tid % 32) ^ (tid / 32 % 2 * 16)) * 8) ^ (64 * m)));
     }
   }
+  // (the second half of a wave takes the dims in the other order of halves: its rows are 8 further, on the
+  // same banks)
+  const int vd4 = (tid % 32) ^ (tid / 32 % 2 * 16);
   auto load_k = [&](int t) {
     const uint8_t *tp = cbase + (int64_t)t * qtile_bytes(D);
 #pragma unroll
@@ -200,8 +203,8 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     const uint8_t *tp = cbase + (int64_t)t * qtile_bytes(D) + qtile_v(D);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      vraw[e] = *(gptr16)(tp + (tid + 128 * e) * 16);
-      const uint2 s = *(const uint2 *)(tp + KT * D / 2 + (((tid / 32) + 4 * e) * 4 + (tid % 32) / 8) * 8);
+      vraw[e] = *(gptr16)(tp + ((tid / 32 + 4 * e) * 32 + vd4) * 16);
+      const uint2 s = *(const uint2 *)(tp + KT * D / 2 + (((tid / 32) + 4 * e) * 4 + vd4 / 8) * 8);
       vsc[e][0] = s.x;
       vsc[e][1] = s.y;
     }

@@ -602,6 +602,35 @@ def test_on_another_stream(ctx):
     step_reference(s)
 
 
+def test_schedule_rotates_its_blocks(hc):
+    """The autoregressive schedule on blocks without positions does what it does on rotated ones."""
+    from paper_2607_20125_amd import ar_loop
+    from synth import inputs as S
+    w = S.WORKLOADS["tiny"]
+    axes, blocks = (24, 20, 20), w.window_blocks + 2
+    data = {(b, i): tuple(normal(1000 + 10 * b + i, 3, w.n_heads, w.block_tokens, w.head_dim)) for b in range(blocks)
+            for i in range(2)}
+    seen = []
+    for rotated in (False, True):
+        ctx = hc.Context(hc.config_from_workload(w, n_layers=1), 0)
+
+        def block(layer, b, step):
+            q, k, v = (t.cuda() for t in data[b, step])
+            if rotated:
+                pos = R.grid_positions(w.block_tokens, w.grid_h, w.grid_w, b * w.frames_per_block)
+                q, k = (ctx.rotate(t.transpose(0, 1).contiguous(), axis_dims=axes, positions=pos.int().cuda())
+                        .transpose(0, 1).contiguous() for t in (q, k))
+            return q, k, v
+
+        out = torch.zeros(w.n_heads, w.block_tokens, w.head_dim, device="cuda")
+        outs = []
+        ar_loop.run(ctx, blocks, block, out, steps=(1000, 500), on_step=lambda *a: outs.append(out.clone()),
+                    tables_at_fill=[[0, 1, 2, 3]], classify=False, axis_dims=None if rotated else axes)
+        seen.append(torch.stack(outs))
+        ctx.close()
+    assert torch.isfinite(seen[0]).all() and torch.equal(seen[0], seen[1])
+
+
 def test_profile_counts(hc):
     c = hc.Context(hc.make_config(n_layers=1), 0)
     s = step_state(c, 500)
