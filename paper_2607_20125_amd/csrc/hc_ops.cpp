@@ -263,10 +263,14 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
   const int64_t keys = p->max_kv > 0 ? std::min(p->max_kv, k->capacity) : k->capacity;
-  // Single tokens: two work groups per CU read one long sequence fastest (131072 tokens of 8 heads: 26 us,
-  // 30 with four, 33 with eight); sequences of different lengths want more and shorter
-  // ranges (48 of them up to 8192: 31 us with 512 groups, 23 with 1024, 19 with 1536 and 2048).
-  if (few_rows) choose_split(a, keys, k->n_seqs == 1 ? 512 : 1536, 4, kDecodeMaxSplit);
+  // Single tokens.  Two work groups per CU read a few long sequences fastest (131072 tokens of 8 heads: 26 us,
+  // 30 with four, 33 with eight; two sequences of 65536: 31, 33 with four, 37 with six).  More sequences are
+  // usually of different lengths and end unevenly, so their ranges are shorter: 48 of up to 8192 tokens (192
+  // units) 31 us with 512 groups, 23 with 1024, 19 with 1536; 8 of up to 32768 (64 units) 47, 44 and 43.
+  // (Equal ones lose by it: 32 of 8192, 256 units, 32 and 36 us.)  512 units fill the card by themselves: 64
+  // sequences of up to 1000 tokens 13 us uncut, 20 in three ranges.
+  const int64_t units = seq_units(a);
+  if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units < 192 ? 1024 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);
   a.wide = k->head_dim == 128 && !few_rows && wide_rows(a, keys);
   cut_last_round(a, keys);
