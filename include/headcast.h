@@ -345,7 +345,7 @@ typedef struct {
   void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; overlaps no input     */
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
   int32_t n_tokens;          /* rows of q and out; 0 does nothing                        */
-  int32_t n_keys;            /* rows of k and v                                          */
+  int32_t n_keys;            /* rows of k and v, at most 2^31 - 65                        */
   int32_t n_seqs;            /* >= 1                                                     */
   int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads                      */
   int32_t head_dim;          /* 64 or 128                                                */

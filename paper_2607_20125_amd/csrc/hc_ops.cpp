@@ -158,6 +158,8 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
     return fail(c, HC_E_INVAL, "n_heads must be a multiple of n_kv_heads");
   if (p->head_dim != 64 && p->head_dim != 128) return fail(c, HC_E_INVAL, "head_dim must be 64 or 128");
   if (p->causal_block < 0) return fail(c, HC_E_INVAL, "causal_block must not be negative");
+  // (the kernels round key counts up to whole tiles in 32 bits; keys of stride 0 take no memory)
+  if (p->n_keys > INT32_MAX - kSeqKeys) return fail(c, HC_E_INVAL, "too many keys for one call");
   if (!p->cu_k && p->n_keys != p->n_tokens)
     return fail(c, HC_E_INVAL, "cu_k is NULL, so n_keys must be n_tokens");
   if (p->cu_k && !aligned4(p->cu_k)) return fail(c, HC_E_INVAL, "cu_k must be 4-byte aligned");

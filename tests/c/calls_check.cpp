@@ -1,0 +1,120 @@
+// More checks of the entry points beside the routed attention (hc_ops.cpp) on the CPU: calls at the
+// ends of their ranges.  As ops_check.cpp, against the HIP runtime of fake_hip.h, but with
+// devices that are told apart.  One check per run, by name.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+#include <functional>
+#include <string>
+
+#include <hip/hip_runtime.h>
+
+#define hipSetDevice ignored_set_device       // (fake_hip.h's looks at no device)
+#include "fake_hip.h"
+#undef hipSetDevice
+#include "hc_ops.h"
+#include "headcast.h"
+
+using namespace hc;
+
+namespace {
+int fails = 0;
+#define CHECK(cond)                                                           \
+  do {                                                                        \
+    if (!(cond)) {                                                            \
+      std::fprintf(stderr, "check failed: %s (line %d)\n", #cond, __LINE__); \
+      ++fails;                                                                \
+    }                                                                         \
+  } while (0)
+
+int device_now = 0;                // the calling thread's
+SeqArgs attended;
+hipError_t launched() {
+  ++fake::launches;
+  return hipSuccess;
+}
+}  // namespace
+
+extern "C" {
+hipError_t hipGetDevice(int *d) { *d = device_now; return hipSuccess; }
+hipError_t hipSetDevice(int d) { device_now = d; return hipSuccess; }
+}
+
+namespace hc {
+hipError_t launch_rotate(const RotateArgs &, int, int, bool, hipStream_t) { return launched(); }
+hipError_t launch_qcache_append(const QCacheArgs &, hipStream_t) { return launched(); }
+hipError_t launch_qcache_read(const QCacheArgs &, hipStream_t) { return launched(); }
+hipError_t launch_seq(const SeqArgs &a, int, hipStream_t) { attended = a; return launched(); }
+hipError_t launch_decode(const SeqArgs &a, int, hipStream_t) { attended = a; return launched(); }
+hipError_t launch_seq_merge(const SeqArgs &, int, int, hipStream_t) { return launched(); }
+}  // namespace hc
+
+namespace {
+
+struct Ctx {
+  hc_ctx *c = nullptr;
+  explicit Ctx(int device = 0) {
+    hc_config cfg;
+    hc_config_default(&cfg);
+    CHECK(hc_create(&cfg, device, &c) == HC_OK);
+  }
+  ~Ctx() { hc_destroy(c); }
+};
+
+alignas(16) char memory[4096];
+const int32_t *const iat = (const int32_t *)memory;
+
+hc_packed_args good_packed() {
+  hc_packed_args p{};
+  p.q = p.k = p.v = memory;
+  p.out = memory + 2048;
+  p.q_token = p.out_token = 64; p.k_token = p.v_token = 64;
+  p.q_head = p.k_head = p.v_head = p.out_head = 64;
+  p.n_tokens = 1; p.n_keys = 1; p.n_seqs = 1;
+  p.n_heads = 1; p.n_kv_heads = 1; p.head_dim = 64;
+  p.cu_k = iat;
+  return p;
+}
+
+// A call is refused with a message and without a launch.
+void refused(hc_ctx *c, const std::function<hc_status()> &call, const char *word) {
+  const int before = fake::launches;
+  CHECK(call() == HC_E_INVAL);
+  CHECK(fake::launches == before);
+  if (!std::strstr(hc_last_error(c), word)) {
+    std::fprintf(stderr, "message '%s' lacks '%s'\n", hc_last_error(c), word);
+    ++fails;
+  }
+}
+
+// The kernels count key tiles in 32 bits: more keys than those hold are refused, though keys of
+// stride 0 need no memory for them; the most that they hold run.
+void key_counts() {
+  Ctx x;
+  hc_packed_args p = good_packed();
+  p.k_token = p.v_token = 0;
+  int64_t bytes = 0;
+  for (int n : {INT32_MAX, INT32_MAX - kSeqKeys + 1}) {
+    p.n_keys = n;
+    refused(x.c, [&] { return hc_packed_attention(x.c, &p, nullptr); }, "keys");
+    refused(x.c, [&] { return hc_packed_workspace(x.c, &p, &bytes); }, "keys");
+  }
+  p.n_keys = INT32_MAX - kSeqKeys;
+  CHECK(hc_packed_workspace(x.c, &p, &bytes) == HC_OK);
+  p.workspace = memory;
+  p.workspace_bytes = bytes;
+  CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_OK && attended.n_keys == p.n_keys);
+}
+
+}  // namespace
+
+int main(int argc, char **argv) {
+  const std::string name = argc > 1 ? argv[1] : "";
+  if (name == "key_counts") key_counts();
+  else return 2;
+  for (const std::string &f : fake::faults) std::fprintf(stderr, "%s\n", f.c_str());
+  if (fails || !fake::faults.empty()) return 1;
+  std::printf("%s: ok\n", name.c_str());
+  return 0;
+}
