@@ -14,6 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libheadcast.so")
 SOURCES = ["hc_runtime.cpp", "hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip",
            "hc_ops.cpp", "hc_rotate.hip", "hc_qcache.hip", "hc_seq.hip", "hc_seq128.hip", "hc_decode.hip"]
+# kernels of the routed attention: finite inputs, and decisions on bit patterns where they overflow
+ROUTED = ("hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip")
 
 
 def hipcc() -> str:
@@ -30,9 +32,10 @@ def build_library(verbose: bool = False) -> str:
     flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
              # keep the compiler from forming packed fp32 instructions
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-             # no NaN is produced on these paths: max needs no NaN canonicalisation
-             "-fno-honor-nans",
              "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
+    # max needs no NaN canonicalisation there.  The operators beside them promise what becomes of a NaN and the
+    # entry points refuse it in arguments, so their comparisons have to hold for it.
+    routed = ["-fno-honor-nans"]
     # MFMA results in vector registers (the online-softmax rescale works on them), except
     # where the accumulators of 64 queries per wave need the other half of the register file
     vgpr_form = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
@@ -51,6 +54,7 @@ def build_library(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory(prefix="headcast_build_") as tdir:
         objs = [os.path.join(tdir, src + ".o") for src in SOURCES]
         cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip") else vgpr_form)
+                + (routed if src in ROUTED else [])
                 + ["-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
         with concurrent.futures.ThreadPoolExecutor(max_workers=len(cmds)) as ex:
             list(ex.map(run, cmds))

@@ -28,9 +28,9 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 // With the value 16 lanes away (the other half of a 32-lane row).
-__device__ __forceinline__ float max_xor16(float x) {
+__device__ __forceinline__ float larger_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float sum_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -138,11 +138,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_attn_kernel(SeqArgs a) 
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[kb][r]);
+      for (int r = 0; r < 4; ++r) mx = larger(mx, s[kb][r]);
     mx *= sl2;
     if (__any(mx > m_run + kRescale)) {
-      mx = max_xor32(max_xor16(mx));
-      const float m_new = fmaxf(m_run, mx);
+      mx = larger_xor32(larger_xor16(mx));
+      const float m_new = larger(m_run, mx);
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

@@ -22,6 +22,16 @@ __device__ __forceinline__ float scale_of(uint32_t codes) {
   return __uint_as_float(B == 3 ? codes >> 1 : codes << (23 - 8 * B));
 }
 
+// The larger of two logits, NaN if one of them is: a row that sees a NaN has no other result, and
+// the instruction for it takes three operands and needs no quieting of its inputs as fmaxf's does
+// (34 instructions more for a tile of 64 keys in seq_attn_kernel).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// With the value 32 lanes away (the other half of a row's keys).
+__device__ __forceinline__ float larger_xor32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // One unit of work: rows row0 .. of a sequence (row r is query r / group).
 struct SeqUnit {
   int seq;

@@ -208,10 +208,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
     }
     float mx = s[0][0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, fmaxf(s[0][r], s[1][r]));
-    mx = max_xor32(mx) * sl2;
+    for (int r = 0; r < 16; ++r) mx = larger(mx, larger(s[0][r], s[1][r]));
+    mx = larger_xor32(mx) * sl2;
     if (__any(mx > m_run + kRescale)) {
-      const float m_new = fmaxf(m_run, mx);
+      const float m_new = larger(m_run, mx);
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;

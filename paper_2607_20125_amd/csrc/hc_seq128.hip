@@ -584,10 +584,10 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       for (int qb = 0; qb < NQB; ++qb) {
         float m = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) m = fmaxf(m, fmaxf(s[0][qb][r], s[1][qb][r]));
-        m = max_xor32(m) * sl2;
+        for (int r = 0; r < 16; ++r) m = larger(m, larger(s[0][qb][r], s[1][qb][r]));
+        m = larger_xor32(m) * sl2;
         if (__any(m > m_run[qb] + kRescale)) {
-          const float m_new = fmaxf(m_run[qb], m);
+          const float m_new = larger(m_run[qb], m);
           const float alpha = __builtin_amdgcn_exp2f(m_run[qb] - m_new);
           m_run[qb] = m_new;
           l_run[qb] *= alpha;

@@ -1,0 +1,113 @@
+"""What the attentions over sequences and over the 4-bit cache make of values that are rare: every kernel and
+every plan of key ranges, several sequences at once, on the GPU against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+import operators_ref as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+BF = torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def ctx(hc):
+    c = hc.Context(hc.make_config(n_layers=1), 0)
+    yield c
+    c.close()
+
+
+def normal(seed, *shape, spread=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * spread).to(BF)
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def offsets(lengths):
+    return ints([0] + np.cumsum(lengths).tolist())
+
+
+def parts(x, lengths):
+    return torch.split(x, list(lengths))
+
+
+def reference(q, k, v, block):
+    """(output, sum p |v|) of one sequence in 64 bits on the GPU."""
+    (n, heads, d), (m, kv_heads, _) = q.shape, k.shape
+    out, mag = torch.zeros(n, heads, d, dtype=torch.float64), torch.zeros(n, heads, d, dtype=torch.float64)
+    if n == 0 or m == 0:
+        return out, mag
+    count = torch.tensor(R.seen(n, m, block), device="cuda").unsqueeze(1)
+    hidden = torch.arange(m, device="cuda") >= count
+    for h in range(heads):
+        kh, w = k[:, h // (heads // kv_heads)].double(), v[:, h // (heads // kv_heads)].double()
+        p = torch.softmax((q[:, h].double() @ kh.T.contiguous() * d ** -0.5).masked_fill_(hidden, -math.inf), -1)
+        p = torch.where(count == 0, 0.0, p)
+        out[:, h], mag[:, h] = (p @ w).cpu(), (p @ w.abs()).cpu()
+    return out, mag
+
+
+def attend(ctx, cached, q, k, v, nq, nk, block, capacity=None):
+    """The attention of all sequences, and the keys and values that it is of (those that a cache stands for)."""
+    out = torch.full_like(q, 9.0)
+    if not cached:
+        return ctx.packed_attention(q, k, v, offsets(nq), offsets(nk), out=out, causal_block=block), k, v
+    cache = ctx.qcache(len(nk), k.shape[1], k.shape[2], capacity or max(nk))
+    cache.data.fill_(255)                        # slots never written read as NaN
+    start, cu = ints([0] * len(nk)), offsets(nk)
+    ctx.qcache_append(cache, k, v, start, cu_seqlens=cu)
+    ks, vs = torch.zeros_like(k), torch.zeros_like(v)
+    ctx.qcache_read(cache, ks, vs, start, cu_seqlens=cu)
+    return ctx.qcache_attention(cache, q, ints(nk), offsets(nq), out=out, causal_block=block), ks, vs
+
+
+# --- values that are not finite -------------------------------------------------------------------
+
+NOT_FINITE = [
+    # cached, queries, keys, key heads, group, dim, capacity: the kernel and its plan
+    (True, [2, 2, 1], [100, 90, 30], 2, 2, 64, None),          # few rows, uncut
+    (True, [2, 2, 1], [100, 90, 30], 2, 2, 128, None),
+    (True, [1, 1, 1], [3000, 4000, 900], 1, 4, 64, None),      # few rows in many ranges
+    (True, [1, 1, 1], [3000, 4000, 900], 1, 4, 128, None),
+    (True, [1, 1, 1], [700, 600, 500], 8, 2, 128, None),       # few rows in a few ranges
+    (True, [100, 70, 90], [200, 300, 100], 2, 2, 64, None),    # waves of 32 rows, uncut
+    (True, [100, 70, 90], [200, 300, 100], 2, 2, 128, None),
+    (True, [100, 70, 90], [2000, 1900, 1100], 2, 2, 64, None),     # ... cut
+    (True, [200, 150, 180], [2000, 1900, 1700], 2, 2, 128, None),  # waves of 64 rows, cut
+    (True, [1300, 1400, 1200], [450, 500, 640], 4, 2, 128, None),  # ... uncut
+    (False, [100, 70, 90], [200, 300, 100], 2, 2, 64, None),
+    (False, [100, 70, 90], [200, 300, 100], 2, 2, 128, None),
+    (False, [100, 70, 90], [2000, 1900, 1100], 2, 2, 64, None),
+    (False, [200, 150, 180], [2000, 1900, 1700], 2, 2, 128, None),
+    (False, [1300, 1400, 1200], [450, 500, 640], 4, 2, 128, None),
+]
+
+
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("case", NOT_FINITE, ids=lambda c: f"{'cached' if c[0] else 'packed'}_q{c[1][0]}_k{c[2][0]}_d{c[5]}")
+def test_values_that_are_not_finite(ctx, case, where):
+    """One value of the second sequence that is not finite: a key gives NaN to the rows of its head, a value to its dim
+    (its 32 dims in a cache); everything else is as it is without."""
+    cached, nq, nk, kv_heads, group, d, capacity = case
+    q = normal(1, sum(nq), kv_heads * group, d)
+    k, v = normal(2, sum(nk), kv_heads, d), normal(3, sum(nk), kv_heads, d)
+    bad = torch.tensor(math.nan if not cached or where == "k" else math.inf, dtype=BF)
+    head, dim = kv_heads - 1, 37
+    (k if where == "k" else v)[nk[0] + nk[1] // 2, head, dim] = bad
+    got, k, v = attend(ctx, cached, q, k, v, nq, nk, 0, capacity)
+    spoiled = torch.zeros(sum(nq), kv_heads * group, d, dtype=torch.bool)
+    dims = slice(0, d) if where == "k" else slice(32, 64) if cached else slice(dim, dim + 1)
+    spoiled[nq[0]:nq[0] + nq[1], head * group:, dims] = True
+    got = got.cpu().double()
+    assert bool(torch.isnan(got[spoiled]).all())
+    k, v = torch.nan_to_num(k, nan=0.0), torch.nan_to_num(v, nan=0.0)
+    refs = [reference(*x, 0) for x in zip(parts(q, nq), parts(k, nk), parts(v, nk))]
+    out, mag = (torch.cat([r[i] for r in refs]) for i in range(2))
+    R.assert_attention(torch.where(spoiled, out, got), out, mag, str(case))
