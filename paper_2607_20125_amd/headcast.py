@@ -12,7 +12,6 @@ import os
 import struct
 
 import numpy as np
-import torch
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libheadcast.so")
 
@@ -192,11 +191,18 @@ _PACK_TENSOR = {1: _packer("@2P4qi4x", HCRotateTensor),
 _PACK_PACKED = _packer("@4P8q7if3Pq", HCPackedArgs)
 _PACK_ROWS = _packer("@2P4qi4x2P", HCQCacheRows)
 _PACK_CACHED = _packer("@2P4q4if4x3Pq", HCQCacheAttentionArgs)
-_BF16 = (torch.bfloat16,)
-_ROTATE_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
-# torch's current stream of a device as a hipStream_t: the short way where torch has it
-_raw_stream = (getattr(torch._C, "_cuda_getCurrentRawStream", None)
-               or (lambda device: torch.cuda.current_stream(device).cuda_stream))
+torch = None                # loaded by the first call that takes tensors or makes a QCache: the host functions need none
+
+
+def _use_torch():
+    global torch, _BF16, _ROTATE_TYPES, _raw_stream
+    import torch as module
+    _BF16 = (module.bfloat16,)
+    _ROTATE_TYPES = {module.bfloat16: BF16, module.float32: F32}
+    # torch's current stream of a device as a hipStream_t: the short way where torch has it
+    _raw_stream = (getattr(module._C, "_cuda_getCurrentRawStream", None)
+                   or (lambda device: module.cuda.current_stream(device).cuda_stream))
+    torch = module
 
 
 class QCache:
@@ -204,6 +210,8 @@ class QCache:
     sequences of up to `capacity` tokens.  `Context.qcache` makes one."""
 
     def __init__(self, n_seqs: int, n_heads: int, head_dim: int, capacity: int, device):
+        if torch is None:
+            _use_torch()
         for name, value in (("n_seqs", n_seqs), ("n_heads", n_heads), ("capacity", capacity)):
             if not 1 <= value < 1 << 31:
                 raise ValueError(f"{name} must be at least 1 and below 2^31, got {value}")
@@ -384,6 +392,8 @@ class Context:
         (bf16 or float32; `x` itself rotates in place), new ones by default.  Positions:
         int32 [axes][tokens], or the (frame, row, column) of the tokens of a `grid` of (height,
         width), the context's by default, from frame `frame0` on.  Returns `out`."""
+        if torch is None:
+            _use_torch()
         pair = isinstance(x, (tuple, list))
         xs = x if pair else (x,)
         if out is None:
@@ -420,6 +430,8 @@ class Context:
         """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
         cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
         None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
+        if torch is None:
+            _use_torch()
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if n_seqs is None:
