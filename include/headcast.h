@@ -306,7 +306,8 @@ enum { HC_BF16 = 0, HC_F32 = 1 };
 typedef struct {
   const void *x;             /* [n_tokens][n_heads][head_dim] by the strides below       */
   void *out;                 /* may be x itself with equal strides and types, and may
-                              * not overlap it otherwise                                 */
+                              * not overlap it otherwise; of two tensors, neither's output
+                              * overlaps the other's input or output                     */
   int64_t x_token, x_head, out_token, out_head;
   int32_t n_heads;           /* >= 1                                                     */
 } hc_rotate_tensor;
@@ -342,7 +343,8 @@ hc_status hc_rotate(hc_ctx *ctx, const hc_rotate_args *args, const hc_rotate_ten
  * any of that sequence's queries, and no other sequence's. */
 typedef struct {
   const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
-  void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; overlaps no input     */
+  void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; may be q itself with
+                              * the same strides, and overlaps no input otherwise        */
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
   int32_t n_tokens;          /* rows of q and out; 0 does nothing                        */
   int32_t n_keys;            /* rows of k and v, at most 2^31 - 65                        */
@@ -389,7 +391,8 @@ hc_status hc_qcache_bytes(const hc_qcache *cache, int64_t *bytes);   /* `data` i
  * step, a ring of blocks).  Async. */
 typedef struct {
   void *k, *v;               /* bf16 [n_tokens][n_heads][head_dim] by the strides below; hc_qcache_append
-                              * only reads them                                          */
+                              * only reads them, hc_qcache_read writes both: then they do not
+                              * overlap                                                  */
   int64_t k_token, k_head, v_token, v_head;
   int32_t n_tokens;          /* 0 does nothing                                           */
   const int32_t *start;      /* device [n_seqs] (4-byte aligned)                          */
@@ -408,7 +411,8 @@ hc_status hc_qcache_read(hc_ctx *ctx, const hc_qcache *cache, const hc_qcache_ro
  * kv_len is clamped to [0, capacity]. */
 typedef struct {
   const void *q;             /* bf16 [n_tokens][n_heads][head_dim]                        */
-  void *out;                 /* bf16, the same shape; does not overlap q                  */
+  void *out;                 /* bf16, the same shape; may be q itself with the same strides,
+                              * and does not overlap it otherwise                        */
   int64_t q_token, q_head, out_token, out_head;
   int32_t n_tokens;          /* 0 does nothing                                           */
   int32_t n_heads;           /* a multiple of the cache's heads                           */

@@ -391,7 +391,8 @@ class Context:
         (queries and keys of the same tokens).  `out`: a tensor or pair of the same shapes
         (bf16 or float32; `x` itself rotates in place), new ones by default.  Positions:
         int32 [axes][tokens], or the (frame, row, column) of the tokens of a `grid` of (height,
-        width), the context's by default, from frame `frame0` on.  Returns `out`."""
+        width), the context's by default, from frame `frame0` on.  The outputs of a pair overlap neither
+        each other nor the other's input.  Returns `out`."""
         if torch is None:
             _use_torch()
         pair = isinstance(x, (tuple, list))
@@ -416,6 +417,10 @@ class Context:
             xp, xt, xh = self._rows("x", t, types)
             op, ot, oh = self._rows("out", o, types, shape)
             tensors += xp, op, xt, xh, ot, oh, shape[1]
+        if n_tensors == 2 and n:
+            x0, o0, x1, o1 = tensors[0], tensors[1], tensors[7], tensors[8]
+            if o0 == o1 or o0 == x1 or o1 == x0:
+                raise ValueError("the outputs of a pair overlap each other, or one the other's input")
         gh, gw = (self.cfg.grid_h, self.cfg.grid_w) if grid is None else grid
         args = _PACK_ROTATE(n, d, types[x_type], types[out_type], n_axes, *axis_dims, *(0,) * (4 - n_axes),
                             bool(halves), bool(joint), bool(inverse), gh, gw, frame0, theta,
@@ -429,7 +434,7 @@ class Context:
                          softmax_scale=0.0, workspace=None, n_seqs=None):
         """hc_packed_attention: attention over sequences packed behind one another.  cu_q,
         cu_k: int32 [n_seqs + 1] offsets of the queries and keys; cu_k None takes cu_q's, cu_q
-        None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q)."""
+        None makes `n_seqs` (1) equal parts.  Returns `out` (bf16, the shape of q; may be q itself)."""
         if torch is None:
             _use_torch()
         if out is None:
@@ -445,6 +450,8 @@ class Context:
         m, kv_heads, kd = ks
         if kd != d:
             raise ValueError(f"k: expected heads of {d} dims, got {tuple(ks)}")
+        if n and (m and (op == kp or op == vp) or op == qp and (n > 1 and ot != qt or heads > 1 and oh != qh)):
+            raise ValueError("out overlaps an input (it may be q itself, with the same strides)")
         args = (qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, n, m, n_seqs, heads, kv_heads, d, causal_block,
                 softmax_scale, self._ints("cu_q", cu_q, (n_seqs + 1,)), self._ints("cu_k", cu_k, (n_seqs + 1,)))
         packed = _PACK_PACKED(*args, 0, 0)
@@ -473,6 +480,8 @@ class Context:
             raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
         if heads != cache.n_heads or d != cache.head_dim:
             raise ValueError(f"k: expected shape [tokens][{cache.n_heads}][{cache.head_dim}], got {tuple(shape)}")
+        if kp == vp and n and fn is lib.hc_qcache_read:
+            raise ValueError("k and v overlap: each is written")
         rows = _PACK_ROWS(kp, vp, kt, kh, vt, vh, n, self._ints("start", start, (cache.n_seqs,)),
                           self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
         status = fn(self._h, cache.desc, rows, _raw_stream(self.device))
@@ -485,13 +494,13 @@ class Context:
         self._cache_rows(lib.hc_qcache_append, "hc_qcache_append", cache, k, v, start, cu_seqlens)
 
     def qcache_read(self, cache: QCache, k, v, start, cu_seqlens=None):
-        """hc_qcache_read: writes the stored values of those slots into k and v."""
+        """hc_qcache_read: writes the stored values of those slots into k and v, two tensors."""
         self._cache_rows(lib.hc_qcache_read, "hc_qcache_read", cache, k, v, start, cu_seqlens)
 
     def qcache_attention(self, cache: QCache, q, kv_len, cu_seqlens=None, out=None, *,
                          causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
         """hc_qcache_attention: attention of q over the first kv_len[s] (int32 [n_seqs]) slots
-        of each sequence of the cache.  Returns `out` (bf16, the shape of q)."""
+        of each sequence of the cache.  Returns `out` (bf16, the shape of q; may be q itself)."""
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         qs = q.shape
@@ -502,6 +511,8 @@ class Context:
             raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
         if d != cache.head_dim:
             raise ValueError(f"q: expected heads of {cache.head_dim} dims, got {tuple(qs)}")
+        if op == qp and (n > 1 and ot != qt or heads > 1 and oh != qh):
+            raise ValueError("out overlaps q (it may be q itself, with the same strides)")
         args = (qp, op, qt, qh, ot, oh, n, heads, causal_block, max_kv, softmax_scale,
                 self._ints("kv_len", kv_len, (cache.n_seqs,)),
                 self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))

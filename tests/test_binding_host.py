@@ -1,7 +1,13 @@
 """What the Python binding does on the host alone."""
+import ctypes
 import os
 import subprocess
 import sys
+
+import pytest
+import torch
+
+from paper_2607_20125_amd import headcast as hc
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -24,3 +30,72 @@ def test_host_functions_need_no_torch():
     run = subprocess.run([sys.executable, "-c", WITHOUT_TORCH], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert run.returncode == 0, run.stderr
     assert run.stdout == "fine\n"
+
+
+# --- tensors that a call writes -----------------------------------------------------------------
+
+@pytest.fixture
+def ctx():
+    """A context without a device: its tensors are the CPU's, and a call that is not refused gets as far as the
+    library, which has no context and says so."""
+    c = hc.Context.__new__(hc.Context)
+    c._h, c.device, c.cfg, c._need = ctypes.c_void_p(), -1, hc.default_config(), ctypes.c_int64()
+    return c
+
+
+def rows(n, heads=2, d=64):
+    return torch.zeros(n, heads, d, dtype=torch.bfloat16)
+
+
+@pytest.fixture(autouse=True)
+def no_stream(monkeypatch):
+    hc._use_torch()
+    monkeypatch.setattr(hc, "_raw_stream", lambda device: 0)
+
+
+def taken(call):
+    """The call passes the binding's checks and reaches the library."""
+    with pytest.raises(hc.HeadCastError):
+        call()
+
+
+def test_a_pair_writes_no_tensor_of_the_other(ctx):
+    q, k, o, p = (rows(4) for _ in range(4))
+    kw = dict(axis_dims=(64,), positions=torch.zeros(1, 4, dtype=torch.int32))
+    for xs, outs in (((q, q), (q, q)), ((q, k), (k, q)), ((q, k), (o, o)), ((q, k), (o, q)), ((q, k), (k, o))):
+        with pytest.raises(ValueError, match="overlap"):
+            ctx.rotate(xs, outs, **kw)
+    for xs, outs in (((q, k), (q, k)), ((q, k), (o, p)), ((q, q), (o, p)), ((q, k), None)):
+        taken(lambda: ctx.rotate(xs, outs, **kw))
+    none = rows(0)
+    taken(lambda: ctx.rotate((none, none), (none, none), axis_dims=(64,), positions=torch.zeros(1, 0, dtype=torch.int32)))
+
+
+def test_attention_writes_no_key_and_no_value(ctx):
+    q, k, v = (rows(4) for _ in range(3))
+    for out in (k, v):
+        with pytest.raises(ValueError, match="overlap"):
+            ctx.packed_attention(q, k, v, out=out)
+    cu = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="overlap"):     # the queries' memory in another order
+        ctx.packed_attention(q[:2], k, v, cu, cu, out=q[:2].transpose(0, 1))
+    taken(lambda: ctx.packed_attention(q, k, k, out=q))
+    taken(lambda: ctx.packed_attention(q, q, q))
+    one = rows(1)
+    taken(lambda: ctx.packed_attention(one, k, v, cu, cu, out=one.as_strided((1, 2, 64), (1, 64, 1))))
+    none = q[:0]
+    taken(lambda: ctx.packed_attention(none, none, none, out=none))
+    cache = hc.QCache(1, 2, 64, 10, "cpu")
+    n = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="overlap"):
+        ctx.qcache_attention(cache, q[:2], n, out=q[:2].transpose(0, 1))
+    taken(lambda: ctx.qcache_attention(cache, q, n, out=q))
+
+
+def test_reading_a_cache_needs_two_tensors(ctx):
+    cache, k, n = hc.QCache(1, 2, 64, 10, "cpu"), rows(4), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="overlap"):
+        ctx.qcache_read(cache, k, k, n)
+    taken(lambda: ctx.qcache_read(cache, k[:0], k[:0], n))
+    taken(lambda: ctx.qcache_read(cache, k, rows(4), n))
+    taken(lambda: ctx.qcache_append(cache, k, k, n))

@@ -111,3 +111,20 @@ def test_values_that_are_not_finite(ctx, case, where):
     refs = [reference(*x, 0) for x in zip(parts(q, nq), parts(k, nk), parts(v, nk))]
     out, mag = (torch.cat([r[i] for r in refs]) for i in range(2))
     R.assert_attention(torch.where(spoiled, out, got), out, mag, str(case))
+
+
+# --- outputs in the queries' place ----------------------------------------------------------------
+
+@pytest.mark.parametrize("case", NOT_FINITE, ids=lambda c: f"{'cached' if c[0] else 'packed'}_q{c[1][0]}_k{c[2][0]}_d{c[5]}")
+def test_outputs_over_the_queries(ctx, case):
+    cached, nq, nk, kv_heads, group, d, _ = case
+    q = normal(11, sum(nq), kv_heads * group, d)
+    k, v = normal(12, sum(nk), kv_heads, d), normal(13, sum(nk), kv_heads, d)
+    if cached:
+        cache = ctx.qcache(len(nk), kv_heads, d, max(nk))
+        ctx.qcache_append(cache, k, v, ints([0] * len(nk)), cu_seqlens=offsets(nk))
+        call = lambda out: ctx.qcache_attention(cache, q, ints(nk), offsets(nq), out=out, causal_block=1)  # noqa: E731
+    else:
+        call = lambda out: ctx.packed_attention(q, k, v, offsets(nq), offsets(nk), out=out, causal_block=1)  # noqa: E731
+    want = call(None)
+    assert call(q) is q and torch.equal(q, want)
