@@ -339,7 +339,10 @@ hc_status hc_rotate(hc_ctx *ctx, const hc_rotate_args *args, const hc_rotate_ten
  *                         causal mask, c = block_tokens lets a block see itself and
  *                         every earlier block.
  * A query that sees nothing gets zeros.  Output rows outside every sequence are
- * left as they were.  A NaN or infinity in a sequence's own keys or values may reach
+ * left as they were.  Probabilities are rounded to bfloat16 for the product with the values, as in
+ * hc_attention; logits, the softmax's maxima and sums (of the rounded probabilities) and the outputs'
+ * sums are float32, rounded once to the output.  Logits may be up to 2^28 in magnitude (times log2 e):
+ * a running maximum is rounded by 2^-24 of itself, and beyond that its rounding nears the range of exp2.  A NaN or infinity in a sequence's own keys or values may reach
  * any of that sequence's queries, and no other sequence's. */
 typedef struct {
   const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
@@ -406,7 +409,7 @@ hc_status hc_qcache_read(hc_ctx *ctx, const hc_qcache *cache, const hc_qcache_ro
 
 /* Attention of new queries over the first kv_len[s] slots of each sequence, with the
  * position and mask rules of hc_packed_attention (m = kv_len[s]).  The keys and values
- * are the stored 4-bit ones; q and the probabilities are bfloat16, sums float32.
+ * are the stored 4-bit ones; roundings and the range of logits are those of hc_packed_attention too.
  * With a ring of blocks (slots not in the order of positions) use causal_block = 0.
  * kv_len is clamped to [0, capacity]. */
 typedef struct {

@@ -128,3 +128,20 @@ def test_outputs_over_the_queries(ctx, case):
         call = lambda out: ctx.packed_attention(q, k, v, offsets(nq), offsets(nk), out=out, causal_block=1)  # noqa: E731
     want = call(None)
     assert call(q) is q and torch.equal(q, want)
+
+
+# --- large logits -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("case", NOT_FINITE, ids=lambda c: f"{'cached' if c[0] else 'packed'}_q{c[1][0]}_k{c[2][0]}_d{c[5]}")
+def test_logits_close_to_2_to_the_28(ctx, case, sign):
+    """Logits of one sign up to 2^27.6 (log2 units) that 32 bits hold exactly, three different ones: a row is the mean of
+    the values whose key is best."""
+    cached, nq, nk, kv_heads, group, d, _ = case
+    q = torch.full((sum(nq), kv_heads * group, d), sign * 2.0 ** 10, dtype=BF, device="cuda")
+    level = torch.tensor([9.0, 10.0, 12.0], device="cuda")[torch.arange(sum(nk), device="cuda") * 7 % 11 % 3]
+    k = (level * 2.0 ** 10)[:, None, None].expand(-1, kv_heads, d).to(BF).contiguous()
+    v = normal(21, sum(nk), kv_heads, d)
+    got, k, v = attend(ctx, cached, q, k, v, nq, nk, 0)
+    refs = [reference(*x, 0) for x in zip(parts(q, nq), parts(k, nk), parts(v, nk))]
+    R.assert_attention(got, *(torch.cat([r[i] for r in refs]) for i in range(2)), str(case))
