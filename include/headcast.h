@@ -342,8 +342,9 @@ hc_status hc_rotate(hc_ctx *ctx, const hc_rotate_args *args, const hc_rotate_ten
  * left as they were.  Probabilities are rounded to bfloat16 for the product with the values, as in
  * hc_attention; logits, the softmax's maxima and sums (of the rounded probabilities) and the outputs'
  * sums are float32, rounded once to the output.  Logits may be up to 2^28 in magnitude (times log2 e):
- * a running maximum is rounded by 2^-24 of itself, and beyond that its rounding nears the range of exp2.  A NaN or infinity in a sequence's own keys or values may reach
- * any of that sequence's queries, and no other sequence's. */
+ * a running maximum is rounded by 2^-24 of itself, and beyond that its rounding nears the range of exp2.
+ * A NaN or infinity in a sequence's own keys or values may reach any of that sequence's queries, and no
+ * other sequence's. */
 typedef struct {
   const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
   void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; may be q itself with

@@ -26,6 +26,8 @@ struct OnDevice {
   }
 };
 
+constexpr float kLog2E = 1.4426950408889634f;
+
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Work groups of a launch dimension, of 256 threads at most: the runtime counts threads in 32 bits.
@@ -62,8 +64,8 @@ hc_status check_output(hc_ctx *c, const Rows &t, int dim) {
 }
 
 hc_status check_scale(hc_ctx *c, float scale) {
-  if (!(scale >= 0.f) || !std::isfinite(scale))
-    return fail(c, HC_E_INVAL, "softmax_scale must be finite and not negative");
+  if (!(scale >= 0.f) || !std::isfinite(scale * kLog2E))
+    return fail(c, HC_E_INVAL, "softmax_scale must be finite (times log2 e too) and not negative");
   return HC_OK;
 }
 
@@ -75,7 +77,7 @@ hc_status check_parts(hc_ctx *c, const char *name, const int32_t *cu, int n_toke
 }
 
 float scale_log2(float scale, int head_dim) {
-  return (scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim)) * 1.4426950408889634f;
+  return (scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim)) * kLog2E;
 }
 
 // Units of R rows that the sequences of a call can have: whole ones, and a partial one each

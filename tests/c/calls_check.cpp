@@ -107,11 +107,33 @@ void key_counts() {
   CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_OK && attended.n_keys == p.n_keys);
 }
 
+// The scale is used times log2(e): what leaves the floats there is refused as if it were infinite.
+void large_scales() {
+  Ctx x;
+  hc_packed_args p = good_packed();
+  hc_qcache k{memory, 1, 1, 64, 64};
+  hc_qcache_attention_args a{};
+  a.q = memory; a.out = memory + 2048;
+  a.q_token = a.out_token = a.q_head = a.out_head = 64;
+  a.n_tokens = 1; a.n_heads = 1; a.kv_len = iat;
+  for (float scale : {3e38f, 2.4e38f}) {
+    p.softmax_scale = a.softmax_scale = scale;
+    refused(x.c, [&] { return hc_packed_attention(x.c, &p, nullptr); }, "softmax_scale");
+    refused(x.c, [&] { return hc_qcache_attention(x.c, &k, &a, nullptr); }, "softmax_scale");
+  }
+  for (float scale : {2.3e38f, 1e-38f, 0.f}) {
+    p.softmax_scale = a.softmax_scale = scale;
+    CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_OK && std::isfinite(attended.scale_log2));
+    CHECK(hc_qcache_attention(x.c, &k, &a, nullptr) == HC_OK && std::isfinite(attended.scale_log2));
+  }
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
   const std::string name = argc > 1 ? argv[1] : "";
   if (name == "key_counts") key_counts();
+  else if (name == "large_scales") large_scales();
   else return 2;
   for (const std::string &f : fake::faults) std::fprintf(stderr, "%s\n", f.c_str());
   if (fails || !fake::faults.empty()) return 1;
