@@ -320,7 +320,7 @@ typedef struct {
   int32_t axis_dims[4];      /* even; their sum is a multiple of 16, at most head_dim     */
   int32_t halves, joint, inverse;
   int32_t grid_h, grid_w, frame0;
-  double theta;              /* > 0, finite                                              */
+  double theta;              /* > 0, finite; angles of positions up to 2^31 finite too   */
   const int32_t *positions;
 } hc_rotate_args;
 

@@ -343,8 +343,10 @@ hc_status hc_rotate(hc_ctx *c, const hc_rotate_args *p, const hc_rotate_tensor *
   for (int i = 0, pair = 0; i < p->n_axes; ++i) {
     const int m = p->joint ? rot : p->axis_dims[i];
     const double step = m > 0 ? std::pow(p->theta, -2.0 / m) : 1.0;
-    for (int j = 0; j < p->axis_dims[i] / 2; ++j, ++pair)
+    for (int j = 0; j < p->axis_dims[i] / 2; ++j, ++pair) {
       a.turns[pair] = (p->joint ? pair : j) == 0 ? per_turn : a.turns[pair - 1] * step;
+      if (!std::isfinite(a.turns[pair] * 0x1p31)) return fail(c, HC_E_INVAL, "theta is too small");
+    }
   }
   OnDevice on(c->device);
   HC_HIP(c, on.status);

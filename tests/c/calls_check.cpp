@@ -29,6 +29,7 @@ int fails = 0;
   } while (0)
 
 int device_now = 0;                // the calling thread's
+RotateArgs rotated;
 SeqArgs attended;
 hipError_t launched() {
   ++fake::launches;
@@ -42,7 +43,7 @@ hipError_t hipSetDevice(int d) { device_now = d; return hipSuccess; }
 }
 
 namespace hc {
-hipError_t launch_rotate(const RotateArgs &, int, int, bool, hipStream_t) { return launched(); }
+hipError_t launch_rotate(const RotateArgs &a, int, int, bool, hipStream_t) { rotated = a; return launched(); }
 hipError_t launch_qcache_append(const QCacheArgs &, hipStream_t) { return launched(); }
 hipError_t launch_qcache_read(const QCacheArgs &, hipStream_t) { return launched(); }
 hipError_t launch_seq(const SeqArgs &a, int, hipStream_t) { attended = a; return launched(); }
@@ -128,12 +129,30 @@ void large_scales() {
   }
 }
 
+// A theta so small that an angle of a far position leaves the doubles is refused.
+void small_thetas() {
+  Ctx x;
+  hc_rotate_args a{};
+  a.n_tokens = 1; a.head_dim = 64; a.n_axes = 1; a.axis_dims[0] = 64; a.positions = iat;
+  hc_rotate_tensor t{memory, memory + 2048, 64, 64, 64, 64, 1};
+  for (double theta : {5e-324, 1e-310, 1e-307}) {
+    a.theta = theta;
+    refused(x.c, [&] { return hc_rotate(x.c, &a, &t, 1, nullptr); }, "theta");
+  }
+  for (double theta : {1e-280, 1e-3, 1.0, 1e300}) {
+    a.theta = theta;
+    CHECK(hc_rotate(x.c, &a, &t, 1, nullptr) == HC_OK);
+    for (int i = 0; i < 32; ++i) CHECK(std::isfinite(rotated.turns[i] * -0x1p31));
+  }
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
   const std::string name = argc > 1 ? argv[1] : "";
   if (name == "key_counts") key_counts();
   else if (name == "large_scales") large_scales();
+  else if (name == "small_thetas") small_thetas();
   else return 2;
   for (const std::string &f : fake::faults) std::fprintf(stderr, "%s\n", f.c_str());
   if (fails || !fake::faults.empty()) return 1;
