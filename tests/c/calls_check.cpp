@@ -135,11 +135,11 @@ void small_thetas() {
   hc_rotate_args a{};
   a.n_tokens = 1; a.head_dim = 64; a.n_axes = 1; a.axis_dims[0] = 64; a.positions = iat;
   hc_rotate_tensor t{memory, memory + 2048, 64, 64, 64, 64, 1};
-  for (double theta : {5e-324, 1e-310, 1e-307}) {
+  for (double theta : {5e-324, 1e-315, 1e-310}) {
     a.theta = theta;
     refused(x.c, [&] { return hc_rotate(x.c, &a, &t, 1, nullptr); }, "theta");
   }
-  for (double theta : {1e-280, 1e-3, 1.0, 1e300}) {
+  for (double theta : {1e-307, 1e-3, 1.0, 1e300}) {   // (1e-307: 4.1e296 turns a step, 8.7e305 at 2^31)
     a.theta = theta;
     CHECK(hc_rotate(x.c, &a, &t, 1, nullptr) == HC_OK);
     for (int i = 0; i < 32; ++i) CHECK(std::isfinite(rotated.turns[i] * -0x1p31));
