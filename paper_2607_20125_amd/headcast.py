@@ -350,13 +350,14 @@ class Context:
     # --- operators beside the routed attention -----------------------------------
     # Tensors are [tokens][heads][head_dim] with any token and head strides that are
     # multiples of 8; a head-major tensor [heads][tokens][head_dim] is passed as
-    # t.transpose(0, 1).
+    # t.transpose(0, 1).  No call records a gradient: a tensor that requires one is refused
+    # where torch records them.
 
     def _rows(self, name, t, dtypes, shape=None):
         """Pointer and strides of a [tokens][heads][head_dim] tensor on this context's device."""
         st = t.stride()
         if (len(st) == 3 and st[2] == 1 and t.dtype in dtypes and t.get_device() == self.device
-                and (shape is None or t.shape == shape)):
+                and (shape is None or t.shape == shape) and not t.requires_grad):
             return t.data_ptr(), st[0], st[1]
         if t.dtype not in dtypes or t.get_device() != self.device:
             raise ValueError(f"{name}: expected {' or '.join(map(str, dtypes))} on cuda:{self.device}, "
@@ -364,6 +365,11 @@ class Context:
         if len(st) != 3 or (shape is not None and t.shape != shape):
             raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[tokens][heads][head_dim]'}, "
                              f"got {tuple(t.shape)}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which this call does not record: detach it, or call under "
+                             "torch.no_grad() (the gradient of rotate is rotate with inverse=True)")
+        if st[2] == 1:
+            return t.data_ptr(), st[0], st[1]
         if t.numel():
             raise ValueError(f"{name}: neighbouring dims of a head must be adjacent in memory")
         return t.data_ptr(), 0, 0

@@ -99,3 +99,24 @@ def test_reading_a_cache_needs_two_tensors(ctx):
     taken(lambda: ctx.qcache_read(cache, k[:0], k[:0], n))
     taken(lambda: ctx.qcache_read(cache, k, rows(4), n))
     taken(lambda: ctx.qcache_append(cache, k, k, n))
+
+
+# --- gradients -----------------------------------------------------------------------------------
+
+def test_no_gradient_is_dropped_in_silence(ctx):
+    """The methods record none: a tensor that requires one is refused where gradients are recorded."""
+    kw = dict(axis_dims=(64,), positions=torch.zeros(1, 4, dtype=torch.int32))
+    cache, n = hc.QCache(1, 2, 64, 10, "cpu"), torch.zeros(1, dtype=torch.int32)
+    calls = (lambda x, y: ctx.rotate(x, **kw), lambda x, y: ctx.rotate((y, x), **kw), lambda x, y: ctx.rotate(y, x, **kw),
+             lambda x, y: ctx.packed_attention(x, y, y), lambda x, y: ctx.packed_attention(y, x, y),
+             lambda x, y: ctx.packed_attention(y, y, x), lambda x, y: ctx.qcache_append(cache, x, y, n),
+             lambda x, y: ctx.qcache_append(cache, y, x, n), lambda x, y: ctx.qcache_attention(cache, x, n))
+    for call in calls:
+        x = rows(4).requires_grad_()
+        with pytest.raises(ValueError, match="gradient"):
+            call(x, rows(4))
+        taken(lambda: call(x.detach(), rows(4)))
+        with torch.no_grad():
+            taken(lambda: call(x, rows(4)))
+        with torch.inference_mode():
+            taken(lambda: call(x, rows(4)))
