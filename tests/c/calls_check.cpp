@@ -28,12 +28,14 @@ int fails = 0;
     }                                                                         \
   } while (0)
 
-int device_now = 0;                // the calling thread's
+int device_now = 0, device_in_launch = -1;      // the calling thread's
+hipError_t launch_result = hipSuccess;
 RotateArgs rotated;
 SeqArgs attended;
 hipError_t launched() {
   ++fake::launches;
-  return hipSuccess;
+  device_in_launch = device_now;
+  return launch_result;
 }
 }  // namespace
 
@@ -146,6 +148,49 @@ void small_thetas() {
   }
 }
 
+// Every call launches on its context's device and leaves the caller's current, whatever the launch returns
+// and however the call ends.
+void call_devices() {
+  Ctx x;
+  hc_rotate_args r{};
+  r.n_tokens = 1; r.head_dim = 64; r.n_axes = 1; r.axis_dims[0] = 64; r.positions = iat; r.theta = 1e4;
+  const hc_rotate_tensor t{memory, memory + 2048, 64, 64, 64, 64, 1};
+  hc_qcache k{memory, 1, 1, 64, 64};
+  hc_qcache_rows rows{memory, memory + 2048, 64, 64, 64, 64, 1, iat, nullptr};
+  hc_qcache_attention_args a{};
+  a.q = memory; a.out = memory + 2048;
+  a.q_token = a.out_token = a.q_head = a.out_head = 64;
+  a.n_tokens = 1; a.n_heads = 1; a.kv_len = iat;
+  hc_packed_args p = good_packed(), many = good_packed();      // whole, and in key ranges
+  many.n_keys = 100000;
+  many.k_token = many.v_token = 0;
+  CHECK(hc_packed_workspace(x.c, &many, &many.workspace_bytes) == HC_OK && many.workspace_bytes > 0);
+  many.workspace = memory;
+  const std::function<hc_status()> calls[] = {
+      [&] { return hc_rotate(x.c, &r, &t, 1, nullptr); },
+      [&] { return hc_packed_attention(x.c, &p, nullptr); },
+      [&] { return hc_packed_attention(x.c, &many, nullptr); },
+      [&] { return hc_qcache_append(x.c, &k, &rows, nullptr); },
+      [&] { return hc_qcache_read(x.c, &k, &rows, nullptr); },
+      [&] { return hc_qcache_attention(x.c, &k, &a, nullptr); },
+  };
+  for (int current : {1, 0, 5})
+    for (hipError_t result : {hipSuccess, hipErrorUnknown}) {
+      launch_result = result;
+      for (const auto &call : calls) {
+        device_now = current;
+        device_in_launch = -1;
+        CHECK(call() == (result == hipSuccess ? HC_OK : HC_E_DEVICE));
+        CHECK(device_in_launch == 0 && device_now == current);
+      }
+    }
+  launch_result = hipSuccess;
+  device_now = 1;
+  p.head_dim = 96;                 // a refused call
+  CHECK(hc_packed_attention(x.c, &p, nullptr) == HC_E_INVAL && device_now == 1);
+  device_now = 0;
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
@@ -153,6 +198,7 @@ int main(int argc, char **argv) {
   if (name == "key_counts") key_counts();
   else if (name == "large_scales") large_scales();
   else if (name == "small_thetas") small_thetas();
+  else if (name == "call_devices") call_devices();
   else return 2;
   for (const std::string &f : fake::faults) std::fprintf(stderr, "%s\n", f.c_str());
   if (fails || !fake::faults.empty()) return 1;

@@ -26,7 +26,7 @@ def calls_check(tmp_path_factory):
     return str(exe)
 
 
-@pytest.mark.parametrize("check", ["key_counts", "large_scales", "small_thetas"])
+@pytest.mark.parametrize("check", ["key_counts", "large_scales", "small_thetas", "call_devices"])
 def test_calls(calls_check, check):
     run = subprocess.run([calls_check, check], capture_output=True, text=True, timeout=120,
                          env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
