@@ -30,7 +30,7 @@ TIMESTEPS = (1000, 750, 500, 250)   # Sec. 5.1: four denoising steps per block
 class LoopResult:
     types: list                                      # per layer: head table in force at the end
     stats: list                                      # per layer: statistics of the classification
-    ms_per_block: list = field(default_factory=list)  # attention (+ appends) per block, all steps
+    ms_per_block: list = field(default_factory=list)  # attention, appends and rotations per block, all steps
     classify_ms: float = 0.0                         # all layers, one-time
     classified_at: int = -1                          # block index of the classification
 
@@ -73,9 +73,10 @@ def run(ctx: hc.Context, n_blocks: int, block_data, out, steps=TIMESTEPS, classi
             for layer in range(NL):
                 q, k, v = block_data(layer, b, si)
                 if axis_dims is not None:
-                    turned = torch.empty_like(q), torch.empty_like(k)
-                    ctx.rotate([t.transpose(0, 1) for t in (q, k)], [t.transpose(0, 1) for t in turned],
-                               axis_dims=axis_dims, frame0=b * cfg.frames_per_block)
+                    with torch.no_grad():        # the schedule records no gradient
+                        turned = torch.empty_like(q), torch.empty_like(k)
+                        ctx.rotate([t.transpose(0, 1) for t in (q, k)], [t.transpose(0, 1) for t in turned],
+                                   axis_dims=axis_dims, frame0=b * cfg.frames_per_block)
                     q, k = turned
                 if tables_at_fill is not None and b == W - 1 and si == 0:
                     kw = torch.cat([held_k[layer][j] for j in range(b)] + [k], dim=1)

@@ -81,12 +81,14 @@ NOT_FINITE = [
     (True, [100, 70, 90], [200, 300, 100], 2, 2, 128, None),
     (True, [100, 70, 90], [2000, 1900, 1100], 2, 2, 64, None),     # ... cut
     (True, [200, 150, 180], [2000, 1900, 1700], 2, 2, 128, None),  # waves of 64 rows, cut
-    (True, [1300, 1400, 1200], [450, 500, 640], 4, 2, 128, None),  # ... uncut
+    (True, [1500, 1400, 1200], [450, 500, 640], 4, 2, 128, None),  # ... uncut
+    (True, [100, 70, 90], [6000, 5000, 5500], 1, 1, 64, None),     # many ranges of whole tiles of rows
+    (False, [100, 70, 90], [6000, 5000, 5500], 1, 1, 128, None),
     (False, [100, 70, 90], [200, 300, 100], 2, 2, 64, None),
     (False, [100, 70, 90], [200, 300, 100], 2, 2, 128, None),
     (False, [100, 70, 90], [2000, 1900, 1100], 2, 2, 64, None),
     (False, [200, 150, 180], [2000, 1900, 1700], 2, 2, 128, None),
-    (False, [1300, 1400, 1200], [450, 500, 640], 4, 2, 128, None),
+    (False, [1500, 1400, 1200], [450, 500, 640], 4, 2, 128, None),
 ]
 
 
@@ -145,3 +147,22 @@ def test_logits_close_to_2_to_the_28(ctx, case, sign):
     got, k, v = attend(ctx, cached, q, k, v, nq, nk, 0)
     refs = [reference(*x, 0) for x in zip(parts(q, nq), parts(k, nk), parts(v, nk))]
     R.assert_attention(got, *(torch.cat([r[i] for r in refs]) for i in range(2)), str(case))
+
+
+def test_schedule_rotates_blocks_that_require_gradients(hc):
+    """The schedule records none, so a block from a model's projections runs as a detached one does."""
+    from paper_2607_20125_amd import ar_loop
+    from synth import inputs as S
+    w = S.WORKLOADS["tiny"]
+    outs = []
+    for grad in (False, True):
+        c = hc.Context(hc.config_from_workload(w, n_layers=1), 0)
+        out = torch.zeros(w.n_heads, w.block_tokens, w.head_dim, device="cuda")
+
+        def block(layer, b, step):
+            return tuple(normal(30 + 3 * b + i, w.n_heads, w.block_tokens, w.head_dim).requires_grad_(grad) for i in range(3))
+
+        ar_loop.run(c, 2, block, out, steps=(1000,), classify=False, axis_dims=(24, 20, 20))
+        outs.append(out)
+        c.close()
+    assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
