@@ -166,3 +166,76 @@ def test_schedule_rotates_blocks_that_require_gradients(hc):
         outs.append(out)
         c.close()
     assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
+
+
+# --- several sequences ------------------------------------------------------------------------------
+
+SEVERAL = [
+    # queries, keys, key heads, group, block: 128-dim heads on waves of 64 rows
+    ([700, 1300, 65], [1900, 3333, 1601], 2, 3, 1),                       # key ranges
+    ([700, 1300, 65], [1900, 3333, 1601], 2, 3, 700),
+    ([400, 0, 800], [2000, 1700, 1999], 2, 1, 0),
+    ([500, 900], [300, 2901], 1, 2, 1),                                   # the first queries see nothing
+    ([100, 300, 700], [0, 2500, 2333], 3, 1, 1),
+    ([2000, 1111, 300, 1500], [2000, 1700, 3999, 1501], 4, 2, 1),         # whole units
+    ([2000, 1111, 300, 1500], [2000, 1700, 3999, 1501], 4, 2, 333),
+    ([2500, 2000], [2003, 1999], 8, 1, 0),
+]
+
+
+@pytest.mark.parametrize("spread", [1.0, 40.0])
+@pytest.mark.parametrize("cached", [False, True])
+@pytest.mark.parametrize("case", SEVERAL, ids=lambda c: "x".join(map(str, c[0])) + f"_h{c[2]}x{c[3]}_b{c[4]}")
+def test_several_long_sequences(ctx, case, cached, spread):
+    """Each against its own reference: places of its rows, keys and ranges."""
+    nq, nk, kv_heads, group, block = case
+    q = normal(41, sum(nq), kv_heads * group, 128, spread=spread)
+    k, v = normal(42, sum(nk), kv_heads, 128), normal(43, sum(nk), kv_heads, 128)
+    got, k, v = attend(ctx, cached, q, k, v, nq, nk, block, max(nk) + 77)
+    for s, x in enumerate(zip(parts(got, nq), parts(q, nq), parts(k, nk), parts(v, nk))):
+        if nq[s]:
+            R.assert_attention(x[0], *reference(*x[1:], block), f"sequence {s}")
+
+
+@pytest.mark.parametrize("cached", [False, True])
+@pytest.mark.parametrize("case", [
+    ([1 + i * 7 % 5 for i in range(1000)], [1 + i * 11 % 90 for i in range(1000)], 1, 2, 64),
+    ([i % 3 for i in range(700)], [i * 13 % 70 for i in range(700)], 2, 1, 128),
+    ([1] * 3000, [1 + i * 17 % 40 for i in range(3000)], 1, 4, 64),
+    ([400] + [1] * 63, [500] + [1 + 3 * i for i in range(63)], 1, 4, 128),      # a prompt beside single tokens
+    ([1] * 20 + [500], [1 + 30 * i for i in range(20)] + [500], 1, 4, 128),
+], ids=lambda c: f"{len(c[0])}x{max(c[0])}_d{c[4]}")
+def test_many_sequences(ctx, case, cached):
+    nq, nk, kv_heads, group, d = case
+    q = normal(51, sum(nq), kv_heads * group, d)
+    k, v = normal(52, sum(nk), kv_heads, d), normal(53, sum(nk), kv_heads, d)
+    got, k, v = attend(ctx, cached, q, k, v, nq, nk, 1)
+    q, k, v = q.cpu(), k.cpu(), v.cpu()
+    refs = [R.attention(*x, 1) for x in zip(parts(q, nq), parts(k, nk), parts(v, nk))]
+    R.assert_attention(got, *(torch.cat([r[i] for r in refs]) for i in range(2)), f"{len(nq)} sequences")
+
+
+# --- scales of a cache's values -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("far", [125, 100])
+@pytest.mark.parametrize("seqs,n,d,what", [(40, 16, 64, "few rows"), (40, 16, 128, "few rows"), (2, 320, 64, "32 rows"),
+                                           (2, 320, 128, "32 rows"), (1, 1600, 128, "64 rows")])
+def test_every_scale_beside_any_other(ctx, seqs, n, d, what, far):
+    """A row that sees one key returns its value exactly, at every scale, whatever scales stand beside it: the
+    kernels leave the codes of neighbouring tokens in bits that the conversion does not look at.  With 2^125 (as
+    accumulators) the 64-row kernel takes its second pass, with 2^100 its first."""
+    total = seqs * n
+    g = torch.Generator(device="cuda")
+    g.manual_seed(61)
+    pick = lambda hi, *shape: torch.randint(0, hi, shape, generator=g, device="cuda")  # noqa: E731
+    k = (2 * pick(2, total, 1, d) - 1).to(BF)              # signs: far apart from one another, and stored as they are
+    steps = torch.tensor([0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device="cuda", dtype=torch.float64)[pick(7, total, 1, d)]
+    steps.unflatten(-1, (-1, 32))[..., 0] = 6.0            # (fixes the scale of the 32 dims)
+    scale = torch.exp2(pick(2 * far + 1, total, 1, d // 32).double() - far).repeat_interleave(32, -1)
+    v = (steps * scale * (2 * pick(2, total, 1, d) - 1)).to(BF)
+    order = torch.cat([torch.randperm(n, generator=g, device="cuda") + s * n for s in range(seqs)])
+    q = k[order] * 64.0                                     # logits 64 d for its key, and less by 300 and more (log2) else
+    cache = ctx.qcache(seqs, 1, d, n)
+    ctx.qcache_append(cache, k, v, ints([0] * seqs))
+    got = ctx.qcache_attention(cache, q, ints([n] * seqs), causal_block=0)
+    assert torch.equal(got, v[order])
