@@ -191,14 +191,17 @@ _PACK_TENSOR = {1: _packer("@2P4qi4x", HCRotateTensor),
 _PACK_PACKED = _packer("@4P8q7if3Pq", HCPackedArgs)
 _PACK_ROWS = _packer("@2P4qi4x2P", HCQCacheRows)
 _PACK_CACHED = _packer("@2P4q4if4x3Pq", HCQCacheAttentionArgs)
+_PACK_WORKSPACE = struct.Struct("@Pq").pack      # their last two fields
 torch = None                # loaded by the first call that takes tensors or makes a QCache: the host functions need none
 
 
 def _use_torch():
-    global torch, _BF16, _ROTATE_TYPES, _raw_stream
+    global torch, _BF16, _ROTATE_TYPES, _ROTATE_NONE, _raw_stream
     import torch as module
     _BF16 = (module.bfloat16,)
-    _ROTATE_TYPES = {module.bfloat16: BF16, module.float32: F32}
+    # code and what the others of the call must be; any other type is refused by the tensor's check
+    _ROTATE_TYPES = {module.bfloat16: (BF16, _BF16), module.float32: (F32, (module.float32,))}
+    _ROTATE_NONE = BF16, (module.bfloat16, module.float32)
     # torch's current stream of a device as a hipStream_t: the short way where torch has it
     _raw_stream = (getattr(module._C, "_cuda_getCurrentRawStream", None)
                    or (lambda device: module.cuda.current_stream(device).cuda_stream))
@@ -222,6 +225,7 @@ class QCache:
             raise HeadCastError(st, f"hc_qcache_bytes: {status_string(st)}")
         self.data = torch.empty(nbytes.value, dtype=torch.uint8, device=device)
         self.desc.data = self.data.data_ptr()
+        self.device = self.data.get_device()
         self.n_seqs, self.n_heads = n_seqs, n_heads
         self.head_dim, self.capacity = head_dim, capacity
 
@@ -412,25 +416,28 @@ class Context:
             raise ValueError("rotate takes one tensor or a pair, and as many outputs")
         if not 1 <= n_axes <= 4:
             raise ValueError("axis_dims must have one to four entries")
-        types = _ROTATE_TYPES
-        n, _, d = xs[0].shape if xs[0].dim() == 3 else (0, 0, -1)
-        x_type, out_type = xs[0].dtype, outs[0].dtype
-        tensors = []
+        x_code, x_types = _ROTATE_TYPES.get(xs[0].dtype, _ROTATE_NONE)
+        out_code, out_types = _ROTATE_TYPES.get(outs[0].dtype, _ROTATE_NONE)
+        tensors, n = [], -1
         for t, o in zip(xs, outs):
             shape = t.shape
-            if t.dtype is not x_type or o.dtype is not out_type or shape[0] != n or shape[-1] != d:
+            xp, xt, xh = self._rows("x", t, x_types)
+            op, ot, oh = self._rows("out", o, out_types, shape)
+            if n < 0:
+                n, heads, d = shape
+            elif shape[0] != n or shape[2] != d:
                 raise ValueError("a pair has the same tokens, dims and types")
-            xp, xt, xh = self._rows("x", t, types)
-            op, ot, oh = self._rows("out", o, types, shape)
-            tensors += xp, op, xt, xh, ot, oh, shape[1]
+            else:
+                heads = shape[1]
+            tensors += xp, op, xt, xh, ot, oh, heads
         if n_tensors == 2 and n:
             x0, o0, x1, o1 = tensors[0], tensors[1], tensors[7], tensors[8]
             if o0 == o1 or o0 == x1 or o1 == x0:
                 raise ValueError("the outputs of a pair overlap each other, or one the other's input")
         gh, gw = (self.cfg.grid_h, self.cfg.grid_w) if grid is None else grid
-        args = _PACK_ROTATE(n, d, types[x_type], types[out_type], n_axes, *axis_dims, *(0,) * (4 - n_axes),
-                            bool(halves), bool(joint), bool(inverse), gh, gw, frame0, theta,
-                            self._ints("positions", positions, (n_axes, n)))
+        args = _PACK_ROTATE(n, d, x_code, out_code, n_axes, *axis_dims, *(0,) * (4 - n_axes),
+                            1 if halves else 0, 1 if joint else 0, 1 if inverse else 0, gh, gw, frame0, theta,
+                            0 if positions is None else self._ints("positions", positions, (n_axes, n)))
         status = lib.hc_rotate(self._h, args, _PACK_TENSOR[n_tensors](*tensors), n_tensors, _raw_stream(self.device))
         if status:
             self._check(status, "hc_rotate")
@@ -446,7 +453,7 @@ class Context:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if n_seqs is None:
-            n_seqs = cu_q.shape[0] - 1 if cu_q is not None else 1
+            n_seqs = 1 if cu_q is None else cu_q.numel() - 1
         qs, ks = q.shape, k.shape
         qp, qt, qh = self._rows("q", q, _BF16)
         kp, kt, kh = self._rows("k", k, _BF16)
@@ -456,18 +463,20 @@ class Context:
         m, kv_heads, kd = ks
         if kd != d:
             raise ValueError(f"k: expected heads of {d} dims, got {tuple(ks)}")
-        if n and (m and (op == kp or op == vp) or op == qp and (n > 1 and ot != qt or heads > 1 and oh != qh)):
+        if op in (qp, kp, vp) and n and (m and op in (kp, vp)
+                                         or op == qp and (n > 1 and ot != qt or heads > 1 and oh != qh)):
             raise ValueError("out overlaps an input (it may be q itself, with the same strides)")
-        args = (qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, n, m, n_seqs, heads, kv_heads, d, causal_block,
-                softmax_scale, self._ints("cu_q", cu_q, (n_seqs + 1,)), self._ints("cu_k", cu_k, (n_seqs + 1,)))
-        packed = _PACK_PACKED(*args, 0, 0)
+        packed = _PACK_PACKED(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, n, m, n_seqs, heads, kv_heads, d,
+                              causal_block, softmax_scale,
+                              0 if cu_q is None else self._ints("cu_q", cu_q, (n_seqs + 1,)),
+                              0 if cu_k is None else self._ints("cu_k", cu_k, (n_seqs + 1,)), 0, 0)
         need = self._need
         status = lib.hc_packed_workspace(self._h, packed, need)
         if status:
             self._check(status, "hc_packed_workspace")
         if need.value:
             workspace = self._work(workspace)
-            packed = _PACK_PACKED(*args, workspace.data_ptr(), workspace.nbytes)
+            packed = packed[:-16] + _PACK_WORKSPACE(workspace.data_ptr(), workspace.nbytes)
         status = lib.hc_packed_attention(self._h, packed, _raw_stream(self.device))
         if status:
             self._check(status, "hc_packed_attention")
@@ -477,19 +486,19 @@ class Context:
         """A new 4-bit cache on this context's device."""
         return QCache(n_seqs, n_heads, head_dim, capacity, f"cuda:{self.device}")
 
-    def _cache_rows(self, fn, what, cache, k, v, start, cu_seqlens):
+    def _cache_rows(self, fn, what, writes, cache, k, v, start, cu_seqlens):
         shape = k.shape
         kp, kt, kh = self._rows("k", k, _BF16)
         vp, vt, vh = self._rows("v", v, _BF16, shape)
         n, heads, d = shape
-        if cache.data.get_device() != self.device:
+        if cache.device != self.device:
             raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
         if heads != cache.n_heads or d != cache.head_dim:
             raise ValueError(f"k: expected shape [tokens][{cache.n_heads}][{cache.head_dim}], got {tuple(shape)}")
-        if kp == vp and n and fn is lib.hc_qcache_read:
+        if writes and kp == vp and n:
             raise ValueError("k and v overlap: each is written")
         rows = _PACK_ROWS(kp, vp, kt, kh, vt, vh, n, self._ints("start", start, (cache.n_seqs,)),
-                          self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
+                          0 if cu_seqlens is None else self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
         status = fn(self._h, cache.desc, rows, _raw_stream(self.device))
         if status:
             self._check(status, what)
@@ -497,11 +506,11 @@ class Context:
     def qcache_append(self, cache: QCache, k, v, start, cu_seqlens=None):
         """hc_qcache_append: stores the rows of k and v (bf16 [tokens][cache heads][head_dim])
         in slots start[s] .. of each sequence (int32 [n_seqs])."""
-        self._cache_rows(lib.hc_qcache_append, "hc_qcache_append", cache, k, v, start, cu_seqlens)
+        self._cache_rows(lib.hc_qcache_append, "hc_qcache_append", False, cache, k, v, start, cu_seqlens)
 
     def qcache_read(self, cache: QCache, k, v, start, cu_seqlens=None):
         """hc_qcache_read: writes the stored values of those slots into k and v, two tensors."""
-        self._cache_rows(lib.hc_qcache_read, "hc_qcache_read", cache, k, v, start, cu_seqlens)
+        self._cache_rows(lib.hc_qcache_read, "hc_qcache_read", True, cache, k, v, start, cu_seqlens)
 
     def qcache_attention(self, cache: QCache, q, kv_len, cu_seqlens=None, out=None, *,
                          causal_block=0, softmax_scale=0.0, max_kv=0, workspace=None):
@@ -513,23 +522,23 @@ class Context:
         qp, qt, qh = self._rows("q", q, _BF16)
         op, ot, oh = self._rows("out", out, _BF16, qs)
         n, heads, d = qs
-        if cache.data.get_device() != self.device:
+        if cache.device != self.device:
             raise ValueError(f"the cache is on {cache.data.device}, not on cuda:{self.device}")
         if d != cache.head_dim:
             raise ValueError(f"q: expected heads of {cache.head_dim} dims, got {tuple(qs)}")
         if op == qp and (n > 1 and ot != qt or heads > 1 and oh != qh):
             raise ValueError("out overlaps q (it may be q itself, with the same strides)")
-        args = (qp, op, qt, qh, ot, oh, n, heads, causal_block, max_kv, softmax_scale,
-                self._ints("kv_len", kv_len, (cache.n_seqs,)),
-                self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)))
-        packed = _PACK_CACHED(*args, 0, 0)
+        packed = _PACK_CACHED(qp, op, qt, qh, ot, oh, n, heads, causal_block, max_kv, softmax_scale,
+                              self._ints("kv_len", kv_len, (cache.n_seqs,)),
+                              0 if cu_seqlens is None else self._ints("cu_seqlens", cu_seqlens, (cache.n_seqs + 1,)),
+                              0, 0)
         need = self._need
         status = lib.hc_qcache_workspace(self._h, cache.desc, packed, need)
         if status:
             self._check(status, "hc_qcache_workspace")
         if need.value:
             workspace = self._work(workspace)
-            packed = _PACK_CACHED(*args, workspace.data_ptr(), workspace.nbytes)
+            packed = packed[:-16] + _PACK_WORKSPACE(workspace.data_ptr(), workspace.nbytes)
         status = lib.hc_qcache_attention(self._h, cache.desc, packed, _raw_stream(self.device))
         if status:
             self._check(status, "hc_qcache_attention")
