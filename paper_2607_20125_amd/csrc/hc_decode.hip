@@ -17,7 +17,8 @@ using namespace dev;
 //    consecutive dims of one key; the dims are contracted in that order, with Q read to match.
 //    Key rows are fed so that lane group g ends up with keys 8 g .. 8 g + 7 of every 32.
 //  * O^T = V^T P^T then needs 8 keys of one dim: the cache keeps V in groups of 8 tokens,
-//    and pairs of converted words give pairs of tokens by one byte permute each.
+//    and pairs of converted words give pairs of tokens by one byte permute each.  The probabilities are
+//    rounded to bf16 for it, and their sum is of the rounded ones (see hc_seq.hip).
 // Measured: 8 key heads of 131072 tokens (143 MB) 26.5 us, 5.4 TB/s, and 4 for the merge; 48 sequences of 1 to 8192
 // tokens with 64-dim heads (52 MB) 20.7 us, where work groups of a few microseconds end unevenly.
 // A second tile ahead, or registers capped for more waves, spills.

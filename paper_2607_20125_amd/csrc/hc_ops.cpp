@@ -259,7 +259,8 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
   a.n_split = 1;
   const int64_t rows = (int64_t)p->n_tokens * a.group;
   // The kernel for few rows reads the cache once per 16 rows and needs no LDS; up to two such
-  // units per sequence it reads no more than the other kernel could hide.
+  // units per sequence it reads no more than the other kernel could hide.  (By the rows of the whole batch, which
+  // is all that the host knows: a prompt of some hundred tokens beside many single ones runs by 16 rows too.)
   few_rows = rows <= (int64_t)k->n_seqs * 2 * kDecodeRows;
   const int R = few_rows ? kDecodeRows : kSeqRows;
   const int64_t tiles = unit_room(p->n_tokens, k->n_seqs, a.group, R, p->cu_seqlens == nullptr);
@@ -269,10 +270,13 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
   const int64_t keys = p->max_kv > 0 ? std::min(p->max_kv, k->capacity) : k->capacity;
   // Single tokens.  Two work groups per CU read a few long sequences fastest (131072 tokens of 8 heads: 26 us,
   // 30 with four, 33 with eight; two sequences of 65536: 31, 33 with four, 37 with six).  More sequences are
-  // usually of different lengths and end unevenly, so their ranges are shorter: 48 of up to 8192 tokens (192
-  // units) 31 us with 512 groups, 23 with 1024, 19 with 1536; 8 of up to 32768 (64 units) 47, 44 and 43.
-  // (Equal ones lose by it: 32 of 8192, 256 units, 32 and 36 us.)  512 units fill the card by themselves: 64
-  // sequences of up to 1000 tokens 13 us uncut, 20 in three ranges.
+  // usually of different lengths and end unevenly, so their ranges are shorter: 48 of up to 8192 tokens, 4 heads,
+  // 31 us with 512 groups, 23 with 1024, 19 with 1536; 8 of up to 32768, 8 heads, 47, 44 and 43.
+  // (Equal ones lose by it: 32 of 8192, 8 heads, 32 and 36 us.)  512 units fill the card by themselves: 64
+  // sequences of up to 1000 tokens, 8 heads, 13 us uncut, 20 in three ranges.
+  // The borders are on the units that the launch has room for.  Where offsets are given those are more than can have
+  // rows: the 48 sequences with 7 query heads to a key head are planned as 276 units and have 192, so
+  // they are cut into 5 ranges, and into 8 where the same single tokens come without offsets.
   const int64_t units = seq_units(a);
   if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units < 192 ? 1024 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);

@@ -13,7 +13,8 @@ using namespace dev;
 // The arithmetic and its order are those of the dense kernel with 64 queries per wave
 // (hc_dense128.hip): a step is 32 slots of two products each (16 of S(t+1) = K(t+1) Q^T, 16
 // of O += V(t) P(t)), each with one pair of probabilities and one operand read three slots
-// ahead, a fixed-offset softmax first and a running max where that does not stand.  What
+// ahead, a fixed-offset softmax first and a running max where that does not stand; probabilities
+// are rounded to bf16 for the products, and the row sums are of the rounded ones (see hc_seq.hip).  What
 // differs:
 //  * Rows are (query, head) pairs, each with its own count of keys, and the tiles that not every row
 //    sees whole run masked, outside the written-out steps.
