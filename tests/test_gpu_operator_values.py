@@ -239,3 +239,92 @@ def test_every_scale_beside_any_other(ctx, seqs, n, d, what, far):
     ctx.qcache_append(cache, k, v, ints([0] * seqs))
     got = ctx.qcache_attention(cache, q, ints([n] * seqs), causal_block=0)
     assert torch.equal(got, v[order])
+
+
+# --- far places and any workspace ----------------------------------------------------------------------
+
+FAR = (1 << 21) + (1 << 14) + 5        # tokens: 8 heads of 128 dims, or 16 of 64, pass 2^31 elements and 2^32 bytes
+
+
+@pytest.mark.parametrize("what", ["queries", "keys"])
+@pytest.mark.parametrize("nq,nk,d", [(300, 500, 64), (300, 500, 128), (200, 1700, 128)])
+def test_packed_rows_behind_32_bit_offsets(ctx, nq, nk, d, what):
+    """One sequence at the end of large tensors, whose other rows belong to none."""
+    heads = 1024 // d
+    at_q, at_k = (FAR, 0) if what == "queries" else (0, FAR)
+    q = torch.empty(at_q + nq, heads, d, dtype=BF, device="cuda")
+    k, v = (torch.empty(at_k + nk, heads, d, dtype=BF, device="cuda") for _ in range(2))
+    q[at_q:], k[at_k:], v[at_k:] = normal(71, nq, heads, d), normal(72, nk, heads, d), normal(73, nk, heads, d)
+    out = torch.empty_like(q)
+    out[max(at_q - 8, 0):at_q] = 9.0
+    ctx.packed_attention(q, k, v, ints([at_q, at_q + nq]), ints([at_k, at_k + nk]), out=out, causal_block=1)
+    assert bool((out[max(at_q - 8, 0):at_q] == 9.0).all())
+    R.assert_attention(out[at_q:], *reference(q[at_q:], k[at_k:], v[at_k:], 1))
+
+
+@pytest.mark.parametrize("rows", [1, 100, 1400])
+@pytest.mark.parametrize("d,capacity", [(64, 1 << 17), (128, 1 << 17), (128, 1000)])
+def test_cached_attention_behind_32_bit_offsets(ctx, d, capacity, rows):
+    """The last sequences of a cache of more than 2^32 bytes; the others are empty.  (1400 rows for each of 3 are
+    more than 32 for each of the 68 or 128 that a long capacity makes: those run on the tile kernels.)"""
+    seqs, heads = (1 << 32) // (2 * capacity * d * 17 // 32) // 4 + 8, 4
+    cache = ctx.qcache(seqs, heads, d, capacity)
+    assert cache.data.numel() > 1 << 32
+    longest = min(capacity, 2000)
+    nk = [0] * (seqs - 3) + [longest, longest // 3, longest - 1]
+    nq = [0] * (seqs - 3) + [rows, rows, rows]
+    k, v = normal(74, sum(nk), heads, d), normal(75, sum(nk), heads, d)
+    start, cu = torch.zeros(seqs, dtype=torch.int32, device="cuda"), offsets(nk)
+    ctx.qcache_append(cache, k, v, start, cu_seqlens=cu)
+    ctx.qcache_read(cache, k, v, start, cu_seqlens=cu)
+    q = normal(76, 3 * rows, 2 * heads, d)
+    got = ctx.qcache_attention(cache, q, ints(nk), offsets(nq), causal_block=1)
+    refs = [reference(*x, 1) for x in zip(parts(q, nq[-3:]), parts(k, nk[-3:]), parts(v, nk[-3:]))]
+    R.assert_attention(got, *(torch.cat([r[i] for r in refs]) for i in range(2)))
+
+
+def test_rotation_and_append_of_rows_behind_32_bit_offsets(ctx):
+    heads, d, n = 8, 128, FAR
+    x = torch.zeros(n, heads, d, dtype=BF, device="cuda")
+    tail = normal(77, 100, heads, d)
+    x[-100:] = tail
+    cache = ctx.qcache(1, heads, d, 100)
+    cu = ints([n - 100, n])
+    ctx.qcache_append(cache, x, x, ints([0]), cu_seqlens=cu)
+    k, v = torch.zeros_like(tail), torch.zeros_like(tail)
+    ctx.qcache_read(cache, k, v, ints([0]))
+    want = R.stored(tail.cpu())
+    assert torch.equal(k.cpu().double(), want) and torch.equal(v.cpu().double(), want)
+    ctx.rotate(x, x, axis_dims=(44, 42, 42), grid=(45, 80), frame0=2)
+    pos = R.grid_positions(n, 45, 80, 2)[:, -100:]
+    ref = R.rotate(tail.cpu(), pos, (44, 42, 42))
+    assert float(tail.abs().max()) < 6
+    # half a step of the output; sines 2.8e-7 and three roundings of 2^-24 of two products of inputs up to 6
+    assert bool(((x[-100:].cpu().double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 12 * (2.8e-7 + 3 * 2.0 ** -24)).all())
+    assert bool((x[:100] == 0).all())
+
+
+@pytest.mark.parametrize("fill", [0, 255, 127])
+@pytest.mark.parametrize("cached,nq,nk,d", [(True, [1, 0, 1], [4000, 900, 3], 128), (True, [90, 100, 1], [3000, 0, 2000], 64),
+                                            (False, [90, 0, 100], [3000, 70, 2000], 128)])
+def test_any_workspace(ctx, cached, nq, nk, d, fill):
+    """What a workspace held before, NaN or large values, reaches no result."""
+    q, k, v = normal(81, sum(nq), 4, d), normal(82, sum(nk), 2, d), normal(83, sum(nk), 2, d)
+    want, _, _ = attend(ctx, cached, q, k, v, nq, nk, 1)
+    work = torch.full((64 << 20,), fill, dtype=torch.uint8, device="cuda")
+    if cached:
+        cache = ctx.qcache(3, 2, d, max(nk))
+        ctx.qcache_append(cache, k, v, ints([0] * 3), cu_seqlens=offsets(nk))
+        got = ctx.qcache_attention(cache, q, ints(nk), offsets(nq), causal_block=1, workspace=work)
+    else:
+        got = ctx.packed_attention(q, k, v, offsets(nq), offsets(nk), causal_block=1, workspace=work)
+    assert torch.equal(got, want) and bool((work != fill).any())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_equal_parts_of_queries_over_keys_by_offsets(ctx, d):
+    nk = [30, 200, 0, 77]
+    q, k, v = normal(84, 4 * 50, 4, d), normal(85, sum(nk), 2, d), normal(86, sum(nk), 2, d)
+    got = ctx.packed_attention(q, k, v, None, offsets(nk), n_seqs=4)
+    refs = [reference(*x, 0) for x in zip(parts(q, [50] * 4), parts(k, nk), parts(v, nk))]
+    R.assert_attention(got, *(torch.cat([r[i] for r in refs]) for i in range(2)))
