@@ -13,8 +13,8 @@ using namespace dev;
 // tile t, and are converted (4-bit codes) and transposed (V) on their way into the
 // other LDS buffer.  Online softmax with lazy rescaling; layouts as in hc_device.h.  Probabilities are
 // rounded to bf16, the operand type of the product with V (wider types run at a fraction of its rate); the row sums
-// add the rounded ones, so that the weights in use add up to 1.  Outputs are 1.0 to 1.7 times as far from 64
-// bits as with probabilities in 32 (two blocks over their text 0.0034 and 0.0019).  Two work groups
+// add the rounded ones, so that the weights in use add up to 1.  Outputs are 1.1 to 1.4 times as far from 64
+// bits as with probabilities in 32 (two blocks over their text 0.0023 and 0.0017 of their size).  Two work groups
 // (three with 64-dim heads: 5% faster where they fill the card) share a CU, a wave each on every SIMD, and hide each
 // other's loads and barriers.  (With S(t+1) computed beside
 // the softmax of tile t, as the dense kernels do, 128-dim heads need more than the 256 registers
