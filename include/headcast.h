@@ -438,16 +438,155 @@ hc_status hc_qcache_workspace(hc_ctx *ctx, const hc_qcache *cache,
 hc_status hc_qcache_attention(hc_ctx *ctx, const hc_qcache *cache,
                               const hc_qcache_attention_args *args, hc_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * A model with a sliding window: the norm before its rotary positions, a cache in pages, and attention that
+ * sees a window and the first tokens, in serving and in training.  The conventions are those of the
+ * operators above.
+ *
+ * The mask.  Query i of n over m keys sits at position p = m - n + i.  With causal_block = c > 0 its keys end
+ * before e = (p / c + 1) c (and before m); there are none if p < 0.  Of these it sees
+ *   the first `sinks`, and those from e - window on (all of them with window = 0).
+ * c = 1 and a window of w tokens: the token and the w - 1 before it.  c = block_tokens and a window of
+ * whole blocks: a block sees itself and the blocks before it that the window holds.  causal_block = 0: every key,
+ * and no window.  A query that sees nothing gets zeros.
+ * ------------------------------------------------------------------------- */
+
+/* Root-mean-square norm of every head, then the rotation of hc_rotate:
+ * y = R (x r w), r = (mean of x^2 over the head's dims + eps)^(-1/2), in 32 bits, rounded once to the output's
+ * type (squares overflow 32 bits from 1.8e19 on).  All dims are normed; those behind the rotated ones are
+ * not turned.  In place as hc_rotate. */
+typedef struct {
+  const void *x;             /* [n_tokens][n_heads][head_dim] by the strides below       */
+  void *out;
+  const void *weight;        /* w: [head_dim], 16-byte aligned, or NULL: ones             */
+  int64_t x_token, x_head, out_token, out_head;
+  int32_t n_heads;           /* >= 1                                                     */
+} hc_norm_tensor;
+
+typedef struct {
+  hc_rotate_args rotate;     /* tokens, dims, types, axes and positions                  */
+  int32_t weight_type;       /* HC_BF16 or HC_F32                                        */
+  float eps;                 /* finite, not negative                                     */
+} hc_norm_args;
+
+/* One or two tensors (queries and keys) of the same tokens in one launch.  Async. */
+hc_status hc_norm_rotate(hc_ctx *ctx, const hc_norm_args *args, const hc_norm_tensor *tensors,
+                         int n_tensors, hc_stream stream);
+
+/* The gradients: dx of x (its type), and dweight = float32 sums over tokens and heads, added up in an order that
+ * the sizes alone decide.  x and w are the forward call's, dout (rotate.out_type) the gradient of its
+ * output.  dx may be x or dout itself with the same type and strides. */
+typedef struct {
+  const void *x, *dout, *weight;
+  void *dx;
+  float *dweight;            /* [head_dim], 16-byte aligned, or NULL: not computed        */
+  int64_t x_token, x_head, dout_token, dout_head, dx_token, dx_head;
+  int32_t n_heads;
+} hc_norm_grad_tensor;
+
+hc_status hc_norm_rotate_workspace(hc_ctx *ctx, const hc_norm_args *args, const hc_norm_grad_tensor *tensors,
+                                   int n_tensors, int64_t *bytes);   /* device pointers are not read */
+hc_status hc_norm_rotate_backward(hc_ctx *ctx, const hc_norm_args *args, const hc_norm_grad_tensor *tensors,
+                                  int n_tensors, void *workspace, int64_t workspace_bytes, hc_stream stream);
+
+/* Keys and values of many sequences in pages: slot i of sequence s is token i % page_tokens of page
+ * table[s][i / page_tokens].  A page outside [0, n_pages) is absent: nothing is stored there, and no query
+ * sees its keys.  (So pages that a window has passed may be given away and their entries set to -1.)
+ * Sequences may share pages that are only read. */
+typedef struct {
+  void *k, *v;               /* bf16 [n_pages][page_tokens][n_heads][head_dim] by the strides below */
+  int64_t k_page, k_token, k_head, v_page, v_token, v_head;
+  int32_t n_pages;           /* >= 1                                                     */
+  int32_t page_tokens;       /* a power of two, 16 to 65536                               */
+  int32_t n_heads, head_dim; /* key heads; 64 or 128                                      */
+} hc_pages;
+
+typedef struct {
+  const int32_t *table;      /* device [n_seqs][max_pages] (4-byte aligned), rows `stride` entries apart */
+  int64_t stride;
+  int32_t n_seqs, max_pages; /* >= 1; a sequence has max_pages * page_tokens slots, at most 2^31 - 65 */
+} hc_page_table;
+
+/* Stores rows of k and v as hc_qcache_append does: rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 go to slots
+ * start[s], start[s] + 1, ... of sequence s; what has no slot or no page is dropped.  Two rows for the same place of
+ * a page: either may remain.  Async. */
+hc_status hc_paged_append(hc_ctx *ctx, const hc_pages *pages, const hc_page_table *table,
+                          const hc_qcache_rows *rows, hc_stream stream);
+
+/* Attention of new queries (a chunk of each sequence, or single tokens) over its first kv_len[s] slots, m =
+ * kv_len[s] in the mask above.  Roundings and the range of logits are those of hc_packed_attention.  Slots behind kv_len
+ * and absent pages are not read. */
+typedef struct {
+  const void *q;             /* bf16 [n_tokens][n_heads][head_dim]                        */
+  void *out;                 /* bf16, the same shape; may be q itself with the same strides,
+                              * and overlaps nothing else                                */
+  int64_t q_token, q_head, out_token, out_head;
+  int32_t n_tokens;          /* 0 does nothing                                           */
+  int32_t n_heads;           /* a multiple of the pages' heads                            */
+  int32_t causal_block, window, sinks;
+  int32_t max_kv;            /* about the longest kv_len, 0 if unknown (see hc_qcache_attention) */
+  float softmax_scale;       /* 0 => 1/sqrt(head_dim)                                    */
+  const int32_t *kv_len;     /* device [n_seqs] (4-byte aligned), clamped to the slots     */
+  const int32_t *cu_seqlens; /* device [n_seqs + 1]; NULL: n_seqs equal parts             */
+  void *workspace;           /* hc_paged_workspace bytes, NULL if that is 0               */
+  int64_t workspace_bytes;
+} hc_paged_args;
+
+hc_status hc_paged_workspace(hc_ctx *ctx, const hc_pages *pages, const hc_page_table *table,
+                             const hc_paged_args *args, int64_t *bytes);
+hc_status hc_paged_attention(hc_ctx *ctx, const hc_pages *pages, const hc_page_table *table,
+                             const hc_paged_args *args, hc_stream stream);
+
+/* Attention over packed sequences, as hc_packed_attention, with the mask above.  `lse`, if not NULL, gets the
+ * logarithm of every row's sum of exponentials, which hc_window_attention_backward takes: float32
+ * [n_heads][n_tokens], -infinity for a query that sees nothing (the sum is of the probabilities as rounded to
+ * bfloat16, so it is off by up to 2^-8). */
+typedef struct {
+  const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
+  void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; may be q itself with
+                              * the same strides, and overlaps no input otherwise        */
+  float *lse;                /* 4-byte aligned                                           */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  int32_t n_tokens, n_keys, n_seqs, n_heads, n_kv_heads, head_dim;   /* as in hc_packed_args */
+  int32_t causal_block, window, sinks;
+  float softmax_scale;
+  const int32_t *cu_q, *cu_k;
+  void *workspace;           /* hc_window_workspace bytes, NULL if that is 0              */
+  int64_t workspace_bytes;
+} hc_window_args;
+
+hc_status hc_window_workspace(hc_ctx *ctx, const hc_window_args *args, int64_t *bytes);
+hc_status hc_window_attention(hc_ctx *ctx, const hc_window_args *args, hc_stream stream);
+
+/* Its gradients.  `forward` holds the forward call's q, k, v, out and lse (all only read here) and sizes; its
+ * workspace is not used.  With p the probabilities and s the scale,
+ *   dv = p^T dout,  ds = p (dout v^T - rowsum(dout out)) s,  dq = ds k,  dk = ds^T q,
+ * summed over the query heads that share a key head.  p and ds are rounded to bfloat16 for the products, sums are
+ * float32, rounded once; repeated calls agree bit for bit.  Rows outside every sequence are left as they were; a key that
+ * no query sees gets zeros.  Async. */
+typedef struct {
+  hc_window_args forward;
+  const void *dout;          /* bf16 [n_tokens][n_heads][head_dim] by the strides below   */
+  void *dq, *dk, *dv;        /* bf16, the shapes of q, k and v; overlap nothing            */
+  int64_t dout_token, dout_head, dq_token, dq_head, dk_token, dk_head, dv_token, dv_head;
+  void *workspace;           /* hc_window_backward_workspace bytes, never 0 for tokens     */
+  int64_t workspace_bytes;
+} hc_window_grad_args;
+
+hc_status hc_window_backward_workspace(hc_ctx *ctx, const hc_window_grad_args *args, int64_t *bytes);
+hc_status hc_window_attention_backward(hc_ctx *ctx, const hc_window_grad_args *args, hc_stream stream);
+
 /* Kernel timing: when enabled, every launch the context makes records a pair
  * of HIP events on the stream it is launched on.  hc_profile_read synchronises
  * those events and returns the summed duration (ms) and the launch count of
  * one kernel kind since the last reset, then resets it.  A merge of partials
  * counts as HC_K_COMBINE; one of Spatial ranges alone is timed with its
- * HC_K_SPATIAL launch.  HC_K_SEQUENCE is hc_packed_attention and
- * hc_qcache_attention (the merge of their key ranges included), HC_K_CACHE hc_qcache_append and
- * hc_qcache_read. */
+ * HC_K_SPATIAL launch.  HC_K_SEQUENCE is hc_packed_attention,
+ * hc_qcache_attention, hc_paged_attention and hc_window_attention (the merge of their key ranges included),
+ * HC_K_CACHE hc_qcache_append, hc_qcache_read and hc_paged_append, HC_K_ROTATE hc_rotate, hc_norm_rotate and its
+ * gradients, HC_K_GRADIENT hc_window_attention_backward. */
 enum { HC_K_DENSE = 0, HC_K_SPATIAL = 1, HC_K_SCATTER = 2, HC_K_STATS = 3, HC_K_COMBINE = 4,
-       HC_K_ROTATE = 5, HC_K_SEQUENCE = 6, HC_K_CACHE = 7, HC_K_COUNT = 8 };
+       HC_K_ROTATE = 5, HC_K_SEQUENCE = 6, HC_K_CACHE = 7, HC_K_GRADIENT = 8, HC_K_COUNT = 9 };
 hc_status hc_profile_enable(hc_ctx *ctx, int on);
 hc_status hc_profile_read(hc_ctx *ctx, int kernel_kind, double *total_ms, int64_t *launches);
 

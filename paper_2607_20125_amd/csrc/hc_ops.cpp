@@ -1,100 +1,10 @@
 // Entry points of the operators beside the routed attention: rotary positions,
 // attention over packed sequences, and the 4-bit cache with its attention.
-#include "hc_ops.h"
-
-#include <algorithm>
-#include <cmath>
-#include <cstdint>
-
-#include "hc_context.h"
+#include "hc_args.h"
 
 using namespace hc;
 
 namespace {
-
-// The context's device is current inside a call, the caller's again behind it.
-struct OnDevice {
-  int before = -1;
-  hipError_t status;
-  explicit OnDevice(int device) {
-    status = hipGetDevice(&before);
-    if (status == hipSuccess && before == device) before = -1;
-    else if (status == hipSuccess) status = hipSetDevice(device);
-  }
-  ~OnDevice() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
-
-constexpr float kLog2E = 1.4426950408889634f;
-
-bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-// Work groups of a launch dimension, of 256 threads at most: the runtime counts threads in 32 bits.
-bool good_grid(int64_t groups) { return groups <= (int64_t)UINT32_MAX / 256; }
-
-// A tensor of rows that are moved as 16-byte vectors.  (The stride of an axis of length 1 says nothing.)
-struct Rows {
-  const char *name;
-  const void *p;
-  int64_t token, head, n_tokens, n_heads;
-};
-hc_status check_tensor(hc_ctx *c, const Rows &t) {
-  if (!t.p || !aligned16(t.p)) return fail(c, HC_E_INVAL, "%s must be a 16-byte aligned device pointer", t.name);
-  auto good = [](int64_t stride, int64_t n) { return n <= 1 || (stride >= 0 && stride % 8 == 0); };
-  if (!good(t.token, t.n_tokens) || !good(t.head, t.n_heads))
-    return fail(c, HC_E_INVAL, "%s: strides must be multiples of 8 and not negative", t.name);
-  return HC_OK;
-}
-
-// A tensor that a call writes: besides, no two of its rows of `dim` values overlap.
-hc_status check_output(hc_ctx *c, const Rows &t, int dim) {
-  hc_status st = check_tensor(c, t);
-  if (st != HC_OK) return st;
-  int64_t end = dim;                           // behind the rows along the shorter stride
-  const bool heads_first = t.n_tokens <= 1 || (t.n_heads > 1 && t.head <= t.token);
-  for (int i = 0; i < 2; ++i) {
-    const bool heads = heads_first == (i == 0);
-    const int64_t n = heads ? t.n_heads : t.n_tokens, stride = heads ? t.head : t.token;
-    if (n <= 1) continue;
-    if (stride < end) return fail(c, HC_E_INVAL, "%s: rows overlap", t.name);
-    end += stride > (INT64_MAX - end) / n ? INT64_MAX - end : (n - 1) * stride;
-  }
-  return HC_OK;
-}
-
-hc_status check_scale(hc_ctx *c, float scale) {
-  if (!(scale >= 0.f) || !std::isfinite(scale * kLog2E))
-    return fail(c, HC_E_INVAL, "softmax_scale must be finite (times log2 e too) and not negative");
-  return HC_OK;
-}
-
-hc_status check_parts(hc_ctx *c, const char *name, const int32_t *cu, int n_tokens, int n_seqs) {
-  if (!cu && n_tokens % n_seqs != 0)
-    return fail(c, HC_E_INVAL, "%s is NULL, and %d tokens are no %d equal parts", name, n_tokens, n_seqs);
-  if (cu && !aligned4(cu)) return fail(c, HC_E_INVAL, "%s must be 4-byte aligned", name);
-  return HC_OK;
-}
-
-float scale_log2(float scale, int head_dim) {
-  return (scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim)) * kLog2E;
-}
-
-// Units of R rows that the sequences of a call can have: whole ones, and a partial one each
-// (exactly that many where all sequences are alike).
-int64_t unit_room(int64_t n_tokens, int64_t n_seqs, int64_t group, int R, bool alike) {
-  if (alike || n_seqs == 1) return n_seqs * ((n_tokens / n_seqs * group + R - 1) / R);
-  return n_tokens * group / R + std::min(n_seqs, n_tokens);
-}
-
-// Key ranges per unit.  A launch of fewer work groups than the card runs at once leaves CUs
-// idle, so key tiles are shared out until about `want` groups run, but no range is
-// shorter than `least` tiles: a partial result costs a write, a read and a merge launch.
-void choose_split(SeqArgs &a, int64_t keys, int64_t want, int64_t least, int64_t most) {
-  const int64_t units = (int64_t)a.tiles * a.kv_heads, tiles = (keys + kSeqKeys - 1) / kSeqKeys;
-  const int64_t cuts = std::min({want / std::max<int64_t>(units, 1), tiles / least, most});
-  a.n_split = cuts < 2 || !good_grid(units * cuts) ? 1 : (int32_t)cuts;
-}
 
 // 128-dim heads: waves of 64 rows, which run the matrix cores better but start slowly and hide
 // nothing of it (one wave per SIMD), or of 32.  9360 rows of 12 heads (900 work groups) over 256, 512 and
@@ -133,22 +43,6 @@ hc_status run_seq(hc_ctx *c, const SeqArgs &a, int head_dim, bool few_rows, hipS
       e = launch_seq_merge(a, head_dim, few_rows ? kDecodeRows : kSeqRows, s);
     return e;
   });
-}
-
-hc_status check_workspace(hc_ctx *c, const void *p, int64_t bytes, int64_t needed) {
-  if (needed == 0) return HC_OK;
-  if (!p || !aligned16(p) || bytes < needed)
-    return fail(c, HC_E_INVAL, "this call needs a 16-byte aligned workspace of %lld bytes", (long long)needed);
-  return HC_OK;
-}
-
-int64_t part_bytes(const SeqArgs &a, int head_dim, int rows) {
-  return seq_cut_units(a) * (16 + a.n_split * seq_part_floats(rows, head_dim) * 4);
-}
-
-void use_workspace(SeqArgs &a, void *p) {
-  a.head = (int32_t *)p;
-  a.part = (float *)((char *)p + seq_cut_units(a) * 16);
 }
 
 // --- packed attention -----------------------------------------------------------------
@@ -295,36 +189,15 @@ hc_status hc_rotate(hc_ctx *c, const hc_rotate_args *p, const hc_rotate_tensor *
   if (!p || !t) return fail(c, HC_E_INVAL, "args or tensors is NULL");
   if (n_tensors != 1 && n_tensors != 2) return fail(c, HC_E_INVAL, "n_tensors must be 1 or 2");
   if (p->n_tokens < 0) return fail(c, HC_E_INVAL, "n_tokens must not be negative");
-  if (p->head_dim < 8 || p->head_dim > kRotMaxDim || p->head_dim % 8 != 0)
-    return fail(c, HC_E_INVAL, "head_dim must be a multiple of 8 up to %d", kRotMaxDim);
-  for (int type : {p->x_type, p->out_type})
-    if (type != HC_BF16 && type != HC_F32) return fail(c, HC_E_INVAL, "types must be HC_BF16 or HC_F32");
-  if (p->n_axes < 1 || p->n_axes > kRotMaxAxes) return fail(c, HC_E_INVAL, "n_axes must be 1 to %d", kRotMaxAxes);
-  if (!(p->theta > 0) || !std::isfinite(p->theta)) return fail(c, HC_E_INVAL, "theta must be positive and finite");
-  RotateArgs a{};
-  int rot = 0;
-  for (int i = 0; i < p->n_axes; ++i) {
-    if (p->axis_dims[i] < 0 || p->axis_dims[i] > p->head_dim || p->axis_dims[i] % 2 != 0)
-      return fail(c, HC_E_INVAL, "axis_dims[%d] must be even and between 0 and head_dim", i);
-    rot += p->axis_dims[i];
-    a.axis_end[i] = rot / 2;
-  }
-  if (rot < 16 || rot > p->head_dim || rot % 16 != 0)
-    return fail(c, HC_E_INVAL, "axis_dims must add up to a multiple of 16 up to head_dim");
-  if (p->positions) {
-    if (!aligned4(p->positions)) return fail(c, HC_E_INVAL, "positions must be 4-byte aligned");
-  } else {
-    if (p->n_axes != 3 || p->grid_h < 1 || p->grid_w < 1)
-      return fail(c, HC_E_INVAL, "positions from the grid need three axes, grid_h and grid_w");
-    const int64_t frames = p->n_tokens / ((int64_t)p->grid_h * p->grid_w) + 1;
-    if (p->frame0 + frames > INT32_MAX) return fail(c, HC_E_INVAL, "frame0 is too large");
-  }
+  RotateArgs a;
+  hc_status st = check_rotation(c, p, a);
+  if (st != HC_OK) return st;
   int64_t heads = 0;
   for (int i = 0; i < n_tensors; ++i) {
     if (t[i].n_heads < 1) return fail(c, HC_E_INVAL, "tensor %d: n_heads must be at least 1", i);
     heads += t[i].n_heads;
     if (p->n_tokens == 0) continue;
-    hc_status st = check_tensor(c, {"x", t[i].x, t[i].x_token, t[i].x_head, p->n_tokens, t[i].n_heads});
+    st = check_tensor(c, {"x", t[i].x, t[i].x_token, t[i].x_head, p->n_tokens, t[i].n_heads});
     if (st == HC_OK)
       st = check_output(c, {"out", t[i].out, t[i].out_token, t[i].out_head, p->n_tokens, t[i].n_heads}, p->head_dim);
     if (st != HC_OK) return st;
@@ -336,22 +209,8 @@ hc_status hc_rotate(hc_ctx *c, const hc_rotate_args *p, const hc_rotate_tensor *
   if (heads > 65535 || !good_grid((int64_t)p->n_tokens * (p->head_dim / 8) / 256 + 1))
     return fail(c, HC_E_INVAL, "too many heads or tokens for one call");
   if (p->n_tokens == 0) return HC_OK;
-  a.positions = p->positions;
-  a.n_tokens = p->n_tokens; a.head_dim = p->head_dim; a.rot = rot;
-  a.n_axes = p->n_axes;
-  a.grid_h = p->grid_h; a.grid_w = p->grid_w; a.frame0 = p->frame0;
   a.heads = (int)heads;
-  a.sign = p->inverse ? -1.f : 1.f;
-  // theta^(-2 j / m) / (2 pi), by repeated products (63 roundings of 2^-53 at most)
-  const double per_turn = 0.15915494309189533577;
-  for (int i = 0, pair = 0; i < p->n_axes; ++i) {
-    const int m = p->joint ? rot : p->axis_dims[i];
-    const double step = m > 0 ? std::pow(p->theta, -2.0 / m) : 1.0;
-    for (int j = 0; j < p->axis_dims[i] / 2; ++j, ++pair) {
-      a.turns[pair] = (p->joint ? pair : j) == 0 ? per_turn : a.turns[pair - 1] * step;
-      if (!std::isfinite(a.turns[pair] * 0x1p31)) return fail(c, HC_E_INVAL, "theta is too small");
-    }
-  }
+  if ((st = plan_rotation(c, p, a)) != HC_OK) return st;
   OnDevice on(c->device);
   HC_HIP(c, on.status);
   return timed_launch(c, (hipStream_t)stream, HC_K_ROTATE, [&] {

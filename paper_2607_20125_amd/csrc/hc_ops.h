@@ -83,6 +83,13 @@ struct SeqArgs {
   float *part;                   // [unit - whole][n_split][rows (d + 2)]
   float scale_log2;              // softmax scale * log2(e)
   bool wide;                     // 128-dim heads: waves of 64 rows (hc_seq128.hip)
+  // attention with a window (hc_window.cpp)
+  int32_t window, sinks;         // window 0: every earlier key
+  float *lse;                    // [heads][n_tokens], or null
+  // the cache in pages: k and v are page 0, `capacity` slots a sequence
+  const int32_t *table;
+  int64_t table_seq, k_page, v_page;
+  int32_t n_pages, page_shift;
 };
 inline int64_t seq_units(const SeqArgs &a) { return (int64_t)a.tiles * a.kv_heads; }
 inline int64_t seq_cut_units(const SeqArgs &a) { return a.n_split > 1 ? seq_units(a) - a.whole : 0; }

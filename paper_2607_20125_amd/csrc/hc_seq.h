@@ -33,6 +33,10 @@ __device__ __forceinline__ float larger_xor32(float x) {
   return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Where a kernel's keys and values are, and its mask: packed tensors or the 4-bit cache, seen up to a count;
+// packed tensors or pages, with a window and first tokens.
+enum class Keys { kPacked, kQuant, kWindow, kPaged };
+
 // One unit of work: rows row0 .. of a sequence (row r is query r / group).
 struct SeqUnit {
   int seq;
@@ -73,14 +77,17 @@ __device__ __forceinline__ SeqSpan seq_span(const SeqArgs &a, int s) {
 // earlier ones, and up to 32 sequences by their keys.  (Ranking costs some 20 vector
 // instructions a sequence and wave.  With units of 16 rows, whose waves share a SIMD by
 // four, that was 5 us a work group for 48 sequences; there they stay in order.)
-template <int R>
+// With BY_KEY the units are runs of R keys instead (group and rows then count keys), earlier ones, which the
+// most queries see, first.
+template <int R, bool BY_KEY = false>
 __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u) {
   SeqSpan p;
   int units, j;
+  auto count = [&](const SeqSpan &x) { return BY_KEY ? x.nk : x.nq * a.group; };
   auto uniform = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };
   if (a.n_seqs == 1) {
     p = seq_span(a, 0);
-    units = (p.nq * a.group + R - 1) / R;
+    units = (count(p) + R - 1) / R;
     j = tile;
     u.seq = 0;
     if (j >= units) return false;
@@ -89,7 +96,7 @@ __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u)
     const int lane = threadIdx.x & 63;
     p = SeqSpan{0, 0, 0, 0};
     if (lane < a.n_seqs) p = seq_span(a, lane);
-    const int mine = (p.nq * a.group + R - 1) / R;
+    const int mine = (count(p) + R - 1) / R;
     int64_t before = 0;
     for (int s = 0; s < a.n_seqs; ++s) {
       const int keys = uniform(p.nk, s), n = uniform(mine, s);
@@ -108,7 +115,7 @@ __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u)
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
       p = SeqSpan{0, 0, 0, 0};
       if (s0 + lane < a.n_seqs) p = seq_span(a, s0 + lane);
-      const int mine = (p.nq * a.group + R - 1) / R;
+      const int mine = (count(p) + R - 1) / R;
       int upto = mine;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
@@ -134,8 +141,8 @@ __device__ __forceinline__ bool seq_unit(const SeqArgs &a, int tile, SeqUnit &u)
   u.q0 = uniform(p.q0, from);
   u.nk = uniform(p.nk, from);
   u.k0 = uniform(p.k0, from);
-  u.rows = u.nq * a.group;
-  u.row0 = (uniform(units, from) - 1 - uniform(j, from)) * R;
+  u.rows = BY_KEY ? u.nk : u.nq * a.group;
+  u.row0 = BY_KEY ? uniform(j, from) * R : (uniform(units, from) - 1 - uniform(j, from)) * R;
   return true;
 }
 

@@ -1,6 +1,6 @@
 // Attention over sequences: packed keys and values in bf16, or the 4-bit cache; and
 // the merge of partial results.
-#include "hc_seq.h"
+#include "hc_mask.h"
 
 namespace hc {
 namespace {
@@ -25,8 +25,9 @@ using namespace dev;
 // ---------------------------------------------------------------------------
 constexpr int kWaves = kSeqRows / 32;
 
-template <int D, bool QUANT>
+template <int D, Keys SRC>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(SeqArgs a) {
+  constexpr bool QUANT = SRC == Keys::kQuant, PAGED = SRC == Keys::kPaged, WINDOW = PAGED || SRC == Keys::kWindow;
   constexpr int KT = kSeqKeys, NKK = D / 16, NDB = D / 32, TILE = KT * D;
   constexpr int NT = 64 * kWaves;
   __shared__ __attribute__((aligned(1024))) uint16_t sK[2][TILE];
@@ -50,11 +51,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) qf[kk] = ld_g16(qp + 16 * kk + 8 * g);
   }
-  const int hi = seen_keys(a, u, qi);
   // keys that every row of the unit sees, and that any row sees (seen_keys grows with the query)
   const int first = u.row0 / a.group, last = min(u.row0 + kSeqRows, u.rows) - 1;
-  const int lo_all = seen_keys(a, u, first), hi_all = seen_keys(a, u, last / a.group);
-  const int nt_all = (hi_all + KT - 1) / KT;
+  int hi = 0, lo_all = 0, hi_all = 0;
+  Seen mine{};
+  KeyTiles tiles(Seen{}, Seen{});
+  if constexpr (WINDOW) {
+    mine = seen_by(a, u, qi);
+    tiles = KeyTiles(seen_by(a, u, first), seen_by(a, u, last / a.group));
+  } else {
+    hi = seen_keys(a, u, qi);
+    lo_all = seen_keys(a, u, first);
+    hi_all = seen_keys(a, u, last / a.group);
+  }
+  const int nt_all = WINDOW ? tiles.n : (hi_all + KT - 1) / KT;
   int t0, t1;
   key_range(a, u, share, nt_all, t0, t1);
   const float sl2 = a.scale_log2;
@@ -78,8 +88,43 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
   const int k_tok = ki / NG, k_grp = ki % NG;
   const int v_grp = vi / (D / 4), v_dim = vi % (D / 4) * 4;
 
+  // pages: the entries of the next tile's runs, read a tile ahead, and the runs without a page of the tile
+  // that is on its way and of the current one
+  int entries = 0;
+  uint32_t absent = 0, absent_now = 0;
   auto load = [&](int t) {
-    if constexpr (QUANT) {
+    if constexpr (PAGED) {
+      const int at = tiles.place(t);
+      absent = absent_runs(a, entries);
+      // run j's first row, less its key's number, so that rows are addressed by their distance from the run
+      auto base = [&](const uint16_t *p, int64_t page, int64_t token, int64_t head_stride, int j) {
+        return p + page_of(a, entries, j) * page + run_token(a, run_of(u, at, j)) * token + head * head_stride;
+      };
+      auto row = [&](int j, int key) { return min(key, u.nk - 1) - run_of(u, at, j) * 16; };
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const int c = tid + i * NT;
+        const int j = D == 128 ? i : 2 * i + wave / 2;
+        kr[i] = gld16(base(a.k, a.k_page, a.k_token, a.k_head, j) + row(j, at * KT + c / (D / 8)) * a.k_token + (c % (D / 8)) * 8);
+      }
+      if (has_v) {
+        const int j0 = D == 128 ? wave : 2 * wave, j1 = D == 128 ? wave : 2 * wave + 1;
+        const uint16_t *p0 = base(a.v, a.v_page, a.v_token, a.v_head, j0);
+        const uint16_t *p1 = D == 128 ? p0 : base(a.v, a.v_page, a.v_token, a.v_head, j1);
+        const uint16_t *p = g ? p1 : p0;
+        const int j = g ? j1 : j0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint2 w = *(const uint2 *)(p + row(j, at * KT + 8 * v_grp + i) * a.v_token + v_dim);
+          vr[i / 2][2 * (i % 2)] = w.x;
+          vr[i / 2][2 * (i % 2) + 1] = w.y;
+        }
+        if (absent >> j & 1)        // any values may stand there: a probability of 0 times 0 is 0
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vr[i] = u32x4{0, 0, 0, 0};
+      }
+      entries = page_entry(a, u, tiles.place(t + 1), lane);
+    } else if constexpr (QUANT) {
       const uint8_t *tp = cbase + (int64_t)t * qtile_bytes(D);
       if (has_k) {
         kr[0] = *(gptr16)(tp + ki * 16);
@@ -92,7 +137,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
         vs[1] = sp[1];
       }
     } else {
-      const int k00 = t * KT;
+      const int k00 = (WINDOW ? tiles.place(t) : t) * KT;
 #pragma unroll
       for (int i = 0; i < KI; ++i) {
         const int c = tid + i * NT;
@@ -185,12 +230,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
   for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
   float m_run = kMInit, l_run = 0.f;
   if (t0 < t1) {
+    if constexpr (PAGED) entries = page_entry(a, u, tiles.place(t0), lane);
     load(t0);
     put(t0);
     __syncthreads();
   }
   for (int t = t0; t < t1; ++t) {
     const int b = t & 1;
+    if constexpr (PAGED) absent_now = absent;
     if (t + 1 < t1) load(t + 1);
     f32x16 s[2] = {f32x16{}, f32x16{}};
 #pragma unroll
@@ -201,7 +248,18 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
             &sK[b][(32 * kb + n) * D + kswz<D>(32 * kb + n, 2 * kk + g) * 8]);
         s[kb] = mfma32(kf, qf[kk], s[kb]);
       }
-    if ((t + 1) * KT > lo_all) {
+    if constexpr (WINDOW) {
+      const int at = tiles.place(t);
+      if (!tiles.whole(at, a.sinks) || absent_now) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = 32 * kb + kperm(8 * (r >> 2) + 4 * g + (r & 3));      // (run key / 16 of the tile)
+            if (!mine.sees(at * KT + key) || (absent_now >> (2 * kb + (r >> 3)) & 1)) s[kb][r] = -INFINITY;
+          }
+      }
+    } else if ((t + 1) * KT > lo_all) {
       const int rem = hi - t * KT;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -263,6 +321,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
         out.put(n, 8 * db + 2 * rq + g, acc[db][4 * rq] * inv, acc[db][4 * rq + 1] * inv, acc[db][4 * rq + 2] * inv,
                 acc[db][4 * rq + 3] * inv);
     out.store(a, u, head, wave * 32, lane);
+    if constexpr (WINDOW)
+      if (a.lse && g == 0 && row < u.rows) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run, l_tot);
   } else {
     const int lrow = wave * 32 + n;
     float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
@@ -313,6 +373,7 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   w.x = __builtin_bit_cast(uint32_t, x);
   w.y = __builtin_bit_cast(uint32_t, y);
   *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = w;
+  if (a.lse && dim == 0) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, l);
 }
 
 // The same for many partial results: a work group takes one row, its threads 4 dims of every
@@ -363,6 +424,7 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   r.x = __builtin_bit_cast(uint32_t, x);
   r.y = __builtin_bit_cast(uint32_t, y);
   *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = r;
+  if (a.lse && dim == 0) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, total);
 }
 
 }  // namespace
@@ -371,11 +433,23 @@ hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
   const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
   if (head_dim == 128 && a.wide) return launch_seq128(a, s);
   if (head_dim == 128) {
-    if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<128, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((seq_attn_kernel<128, false>), grid, block, 0, s, a);
+    if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kQuant>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kPacked>), grid, block, 0, s, a);
   } else {
-    if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<64, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((seq_attn_kernel<64, false>), grid, block, 0, s, a);
+    if (a.cache) hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kQuant>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kPacked>), grid, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_window(const SeqArgs &a, int head_dim, hipStream_t s) {
+  const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
+  if (head_dim == 128) {
+    if (a.table) hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kPaged>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kWindow>), grid, block, 0, s, a);
+  } else {
+    if (a.table) hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kPaged>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kWindow>), grid, block, 0, s, a);
   }
   return hipGetLastError();
 }
