@@ -29,54 +29,57 @@ __device__ __forceinline__ int tswz(int r, int c) {
   return c ^ (D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3));
 }
 
-// What a row needs besides its dims: the logarithm of its sum in log2 units, rowsum(dO O), and its keys.
-struct RowStats {
-  float lse[kTile], delta[kTile];
-  int end[kTile], start[kTile];
-};
-
+// Streamed tiles in LDS: two of each of two tensors.  Addresses are a lane's own part, and constants.
 template <int D>
 struct Streamed {
-  uint16_t x[kTile * D];
-  // A operand of a score product: 16 dims kk of row kperm(n) of 32-row block b
-  __device__ __forceinline__ bf16x8 row(int b, int kk, int n, int g) const {
-    const int r = 32 * b + kperm(n);
-    return *reinterpret_cast<const bf16x8 *>(&x[r * D + tswz<D>(r, 2 * kk + g) * 8]);
+  static constexpr int BYTES = kTile * D * 2;
+  uint16_t x[2][2][kTile * D];         // [buffer][tensor]
+};
+using lds8 = const __attribute__((address_space(3))) bf16x8 *;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+using ldst = __attribute__((address_space(3))) s16x4 *;
+
+template <int D>
+struct Reader {
+  uint32_t row, turn, turn4;           // of a lane, in bytes
+  __device__ __forceinline__ explicit Reader(int lane) {
+    const int n = lane & 31, g = lane >> 5, gl = lane >> 4, i = lane & 15;
+    row = (uint32_t)(kperm(n) * D * 2 + tswz<D>(kperm(n), g) * 16);
+    const int r = 8 * (gl / 2) + i / 4, chunk = 2 * (gl % 2) + (i % 4) / 2;
+    turn = (uint32_t)(r * D * 2 + tswz<D>(r, chunk) * 16 + (i % 2) * 8);
+    turn4 = (uint32_t)((r + 4) * D * 2 + tswz<D>(r + 4, chunk) * 16 + (i % 2) * 8);
   }
-  // A operand of a second product: dims 32 db .. + 31 of rows 16 c .. + 15
-  __device__ __forceinline__ bf16x8 turned(int c, int db, int lane) const {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    using ldst = __attribute__((address_space(3))) s16x4 *;
-    const int gl = lane >> 4, i = lane & 15;
-    const int r = 16 * c + 8 * (gl / 2) + i / 4, chunk = 4 * db + 2 * (gl % 2) + (i % 4) / 2;
-    const uint32_t base = (uint32_t)(uintptr_t)(lvoid)x;
-    const uint32_t at = base + (uint32_t)(r * D + tswz<D>(r, chunk) * 8 + (i % 2) * 4) * 2;
-    const uint32_t at4 = base + (uint32_t)((r + 4) * D + tswz<D>(r + 4, chunk) * 8 + (i % 2) * 4) * 2;
+  // A operand of a score product: 16 dims kk of rows kperm(n) of the 32 at `tile`
+  __device__ __forceinline__ bf16x8 score(uint32_t tile, int kk) const {
+    return *(lds8)(uintptr_t)((row ^ (uint32_t)(32 * kk)) + tile);
+  }
+  // A operand of a second product: dims 32 db .. + 31 of the 16 rows at `tile`
+  __device__ __forceinline__ bf16x8 turned(uint32_t tile, int db) const {
     struct { s16x4 a, b; } w;
-    w.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)at);
-    w.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)at4);
+    w.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((turn ^ (uint32_t)(64 * db)) + tile));
+    w.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((turn4 ^ (uint32_t)(64 * db)) + tile));
     return __builtin_bit_cast(bf16x8, w);
   }
 };
 
-// A tile on its way: rows first .. first + 63 (those behind the last repeat it) of one head.
+// Copies a tile to LDS by DMA: rows first .. first + 63 (those behind the last repeat it) of one head.  Instruction j
+// of wave w moves 1 KB, the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its
+// 16 bytes.  (The base is 4 KB low, so that no offset goes below zero when 1024 j is taken off.)
 template <int D>
-struct Loader {
-  static constexpr int N = kTile * D / 8 / kThreads;     // 16-byte pieces of a thread
-  u32x4 w[N];
-  __device__ __forceinline__ void load(const uint16_t *p, int64_t token, int first, int last) {
+struct Copier {
+  static constexpr int RW = 512 / D, N = kTile / RW / kWaves;     // rows of an instruction, instructions of a wave
+  int lane, wave;
+  // p: the tile's first row; left: rows from there on.  (A row's offset stays below 2^31: token strides are below 2^24.)
+  __device__ __forceinline__ void copy(const uint16_t *p, int64_t token, int left, uint16_t *tile) const {
+    int l = lane;
+    asm volatile("" : "+v"(l));      // (the rest is computed at each copy: kept in registers it makes others spill)
+    const int row = N * wave * RW + l / (D / 8);
+    uint32_t a[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * kThreads;
-      w[i] = gld16(p + min(first + c / (D / 8), last) * token + (c % (D / 8)) * 8);
-    }
-  }
-  __device__ __forceinline__ void put(Streamed<D> &t) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * kThreads, r = c / (D / 8);
-      *reinterpret_cast<u32x4 *>(&t.x[r * D + tswz<D>(r, c % (D / 8)) * 8]) = w[i];
-    }
+    for (int j = 0; j < N; ++j)
+      a[j] = (uint32_t)min(row + j * RW, left - 1) * (uint32_t)token * 2u +
+             (uint32_t)(tswz<D>(row + j * RW, l % (D / 8)) * 16 + 4096 - 1024 * j);
+    lds_dma16_run<N>(p - 2048, a, lds_addr(tile + wave * N * 512));
   }
 };
 
@@ -104,9 +107,24 @@ __global__ __launch_bounds__(256) void grad_stats_kernel(GradArgs a) {
   for (int d = 1; d < C; d *= 2) sum += __shfl_xor(sum, d);
   if (live && c == 0) {
     const int64_t at = (int64_t)h * a.seq.n_tokens + row;
-    a.stats[2 * at] = a.lse[at] * 1.4426950408889634f;
-    a.stats[2 * at + 1] = sum;
+    a.stats[at] = a.lse[at] * 1.4426950408889634f;
+    a.stats[(int64_t)heads * a.seq.n_tokens + at] = sum;
   }
+}
+
+// 64 words to LDS by DMA, word i of the `left` behind p (the last repeats) to place i.
+__device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uint32_t lds) {
+  uint32_t saved;
+  const uint32_t at = (uint32_t)min(lane, left - 1) * 4u;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 4\n\t"
+      "global_load_lds_dword %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(at), "s"(p), "s"(lds)
+      : "memory");
 }
 
 // P and dS of 8 rows as matrix operands
@@ -117,11 +135,10 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 
 // --- dK and dV: a work group takes 128 keys of a key head, each wave 32 --------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void grad_keys_kernel(GradArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void grad_keys_kernel(GradArgs a) {
   constexpr int NKK = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sQ[2];
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sO[2];
-  __shared__ RowStats sR[2];
+  __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // queries, output gradients
+  __shared__ __attribute__((aligned(1024))) float sR[2][2][kTile]; // logarithms, rowsum(dO O)
   const SeqArgs &q = a.seq;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
@@ -131,20 +148,25 @@ __global__ __launch_bounds__(kThreads, 1) void grad_keys_kernel(GradArgs a) {
   SeqUnit u;
   if (!seq_unit<kGradKeys, true>(q, tile, u)) return;
   const int k0 = u.row0, k_last = min(k0 + kGradKeys, u.nk) - 1;
+  const int key = k0 + 32 * wave + n;
 
-  // the queries that see any of the keys
-  int first = 0, end = u.nq;
-  if (q.block) {
-    const int64_t off = (int64_t)u.nk - u.nq;          // position of query 0
-    first = (int)min(max((int64_t)(k0 / q.block) * q.block - off, (int64_t)0), (int64_t)u.nq);
-    if (q.window && k0 >= q.sinks)
-      end = (int)min(max(((int64_t)k_last + q.window) / q.block * q.block - off, (int64_t)first), (int64_t)u.nq);
-  }
-  const int nt = (end - first + kTile - 1) / kTile;    // of every query head
+  // The queries that see a key are a run of them: from its block's first on, and (but for the first tokens) before the block
+  // whose window begins behind it.
+  const int64_t off = (int64_t)u.nk - u.nq;          // position of query 0
+  auto from = [&](int j) {
+    return q.block ? (int)min(max((int64_t)((uint32_t)j / (uint32_t)q.block * (uint32_t)q.block) - off, (int64_t)0), (int64_t)u.nq) : 0;
+  };
+  auto until = [&](int j) {
+    if (q.block == 0 || q.window == 0 || j < q.sinks) return u.nq;
+    const uint32_t e = ((uint32_t)j + (uint32_t)q.window) / (uint32_t)q.block * (uint32_t)q.block;
+    return (int)min(max((int64_t)e - off, (int64_t)0), (int64_t)u.nq);
+  };
+  const int first = from(k0), end = max(first, k0 < q.sinks ? u.nq : until(k_last));
+  const int nt = (end - first + kTile - 1) / kTile;    // tiles of every query head
   const int64_t items = (int64_t)nt * q.group;
   const int i0 = (int)(items * split / a.n_split), i1 = (int)(items * (split + 1) / a.n_split);
+  const int lo = from(min(key, u.nk - 1)), hi = until(min(key, u.nk - 1));
 
-  const int key = k0 + 32 * wave + n;
   bf16x8 kf[NKK], vf[NKK];
   {
     const int64_t row = u.k0 + min(key, u.nk - 1);
@@ -159,50 +181,40 @@ __global__ __launch_bounds__(kThreads, 1) void grad_keys_kernel(GradArgs a) {
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = f32x16{};
 
-  Loader<D> lq, lo;
-  float2 st = {0.f, 0.f};
-  Seen seen{};
-  auto load = [&](int item) {
+  const Copier<D> copier{lane, wave};
+  const Reader<D> reader(lane);
+  const int64_t plane = (int64_t)q.n_tokens * q.kv_heads * q.group;
+  auto load = [&](int item, int b) {
     const int h = head * q.group + item / nt, r0 = first + item % nt * kTile;
-    lq.load(q.q + u.q0 * q.q_token + h * q.q_head, q.q_token, r0, u.nq - 1);
-    lo.load(a.dout + u.q0 * a.do_token + h * a.do_head, a.do_token, r0, u.nq - 1);
-    if (tid < kTile) {
-      const int i = r0 + tid;
-      seen = i < u.nq ? seen_by(q, u, i) : Seen{0, 0, 0};
-      st = *(const float2 *)(a.stats + 2 * ((int64_t)h * q.n_tokens + u.q0 + min(i, u.nq - 1)));
-    }
+    copier.copy(q.q + (u.q0 + r0) * q.q_token + h * q.q_head, q.q_token, u.nq - r0, sT.x[b][0]);
+    copier.copy(a.dout + (u.q0 + r0) * a.do_token + h * a.do_head, a.do_token, u.nq - r0, sT.x[b][1]);
+    if (wave < 2)
+      lds_dma4(a.stats + wave * plane + (int64_t)h * q.n_tokens + u.q0 + r0, u.nq - r0, lane, lds_addr(sR[b][wave]));
   };
-  auto put = [&](int b) {
-    lq.put(sQ[b]);
-    lo.put(sO[b]);
-    if (tid < kTile) {
-      sR[b].lse[tid] = st.x;
-      sR[b].delta[tid] = st.y;
-      sR[b].end[tid] = seen.end;
-      sR[b].start[tid] = seen.start;
-    }
+  // what this wave has in flight has arrived, and then what every wave had
+  auto arrived = [&] {
+    wait_vmcnt<0>();
+    __syncthreads();
   };
   if (i0 < i1) {
-    load(i0);
-    put(0);
-    __syncthreads();
+    load(i0, 0);
+    arrived();
   }
+  const uint32_t tiles = (uint32_t)(uintptr_t)(lvoid)&sT;
   for (int item = i0; item < i1; ++item) {
     const int b = (item - i0) & 1;
-    if (item + 1 < i1) load(item + 1);
+    if (item + 1 < i1) load(item + 1, b ^ 1);
     const int r0 = first + item % nt * kTile;
-    const int wk0 = k0 + 32 * wave, wk1 = min(wk0 + 31, u.nk - 1);
-    const Seen lo_seen = seen_by(q, u, r0), hi_seen = seen_by(q, u, min(r0 + kTile, u.nq) - 1);
-    const bool any = wk0 <= k_last && wk0 < hi_seen.end && (wk0 < q.sinks || wk1 >= lo_seen.start);
-    const bool whole = r0 + kTile <= u.nq && wk1 < lo_seen.end && (wk1 < q.sinks || wk0 >= hi_seen.start);
-    if (any) {
-#pragma unroll
+    if (__any(r0 < hi && r0 + kTile > lo)) {
+      const bool whole = __all(r0 >= lo && r0 + kTile <= hi);
+#pragma unroll 1
       for (int qb = 0; qb < 2; ++qb) {
+        const uint32_t tq = tiles + (uint32_t)(b * 2 * Streamed<D>::BYTES + qb * 32 * D * 2), to = tq + Streamed<D>::BYTES;
         f32x16 s = {}, t = {};
 #pragma unroll
         for (int kk = 0; kk < NKK; ++kk) {
-          s = mfma32(sQ[b].row(qb, kk, n, g), kf[kk], s);
-          t = mfma32(sO[b].row(qb, kk, n, g), vf[kk], t);
+          s = mfma32(reader.score(tq, kk), kf[kk], s);
+          t = mfma32(reader.score(to, kk), vf[kk], t);
         }
         u32x4 pf[2], df[2];
 #pragma unroll
@@ -210,14 +222,15 @@ __global__ __launch_bounds__(kThreads, 1) void grad_keys_kernel(GradArgs a) {
           const int at = 32 * qb + 16 * c + 8 * g;         // the 8 rows of this lane
           float p[8], d[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -sR[b].lse[at + e]));
-            if (!whole) {
-              const int x = sR[b].end[at + e], y = sR[b].start[at + e];
-              if (!(key < x && (key < q.sinks || key >= y))) p[e] = 0.f;
+          for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -sR[b][0][at + e]));
+          if (!whole)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int i = r0 + at + e;
+              if (i < lo || i >= hi) p[e] = 0.f;
             }
-            d[e] = p[e] * (t[8 * c + e] - sR[b].delta[at + e]);
-          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[e] = p[e] * (t[8 * c + e] - sR[b][1][at + e]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             pf[c][e] = pack2(p[2 * e], p[2 * e + 1]);
@@ -228,15 +241,12 @@ __global__ __launch_bounds__(kThreads, 1) void grad_keys_kernel(GradArgs a) {
         for (int c = 0; c < 2; ++c)
 #pragma unroll
           for (int db = 0; db < NDB; ++db) {
-            dv[db] = mfma32(sO[b].turned(2 * qb + c, db, lane), __builtin_bit_cast(bf16x8, pf[c]), dv[db]);
-            dk[db] = mfma32(sQ[b].turned(2 * qb + c, db, lane), __builtin_bit_cast(bf16x8, df[c]), dk[db]);
+            dv[db] = mfma32(reader.turned(to + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, pf[c]), dv[db]);
+            dk[db] = mfma32(reader.turned(tq + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, df[c]), dk[db]);
           }
       }
     }
-    if (item + 1 < i1) {
-      put(b ^ 1);
-      __syncthreads();
-    }
+    if (item + 1 < i1) arrived();
   }
 
   // lane: key n of the wave, dims 32 db + 8 rq + 4 g .. + 3
@@ -299,10 +309,9 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradArgs a) {
 
 // --- dQ: a work group takes 128 queries of a query head, each wave 32 ------------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, 1) void grad_queries_kernel(GradArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void grad_queries_kernel(GradArgs a) {
   constexpr int NKK = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sK[2];
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sV[2];
+  __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // keys, values
   SeqArgs q = a.seq;
   const int group = q.group;
   q.group = 1;                       // rows are the queries of one head
@@ -325,33 +334,40 @@ __global__ __launch_bounds__(kThreads, 1) void grad_queries_kernel(GradArgs a) {
       of[kk] = ld_g16(op + 16 * kk);
     }
   }
-  const float2 st = *(const float2 *)(a.stats + 2 * ((int64_t)h * q.n_tokens + u.q0 + at));
+  const float *sp = a.stats + (int64_t)h * q.n_tokens + u.q0 + at;
+  const float lse = sp[0], delta = sp[(int64_t)q.n_tokens * heads];
   f32x16 dq[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dq[db] = f32x16{};
-  Loader<D> lk, lv;
+  const Copier<D> copier{lane, wave};
+  const Reader<D> reader(lane);
   const uint16_t *kp = q.k + u.k0 * q.k_token + head * q.k_head, *vp = q.v + u.k0 * q.v_token + head * q.v_head;
-  auto load = [&](int t) {
-    lk.load(kp, q.k_token, tiles.place(t) * kTile, u.nk - 1);
-    lv.load(vp, q.v_token, tiles.place(t) * kTile, u.nk - 1);
+  auto load = [&](int t, int b) {
+    const int64_t at = (int64_t)tiles.place(t) * kTile;
+    copier.copy(kp + at * q.k_token, q.k_token, u.nk - (int)at, sT.x[b][0]);
+    copier.copy(vp + at * q.v_token, q.v_token, u.nk - (int)at, sT.x[b][1]);
+  };
+  auto arrived = [&] {
+    wait_vmcnt<0>();
+    __syncthreads();
   };
   if (tiles.n > 0) {
-    load(0);
-    lk.put(sK[0]);
-    lv.put(sV[0]);
-    __syncthreads();
+    load(0, 0);
+    arrived();
   }
+  const uint32_t base = (uint32_t)(uintptr_t)(lvoid)&sT;
   for (int t = 0; t < tiles.n; ++t) {
     const int b = t & 1, place = tiles.place(t);
-    if (t + 1 < tiles.n) load(t + 1);
+    if (t + 1 < tiles.n) load(t + 1, b ^ 1);
     const bool whole = tiles.whole(place, q.sinks);
-#pragma unroll
+#pragma unroll 1
     for (int kb = 0; kb < 2; ++kb) {
+      const uint32_t tk = base + (uint32_t)(b * 2 * Streamed<D>::BYTES + kb * 32 * D * 2), tv = tk + Streamed<D>::BYTES;
       f32x16 s = {}, d = {};
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
-        s = mfma32(sK[b].row(kb, kk, n, g), qf[kk], s);
-        d = mfma32(sV[b].row(kb, kk, n, g), of[kk], d);
+        s = mfma32(reader.score(tk, kk), qf[kk], s);
+        d = mfma32(reader.score(tv, kk), of[kk], d);
       }
       u32x4 df[2];
 #pragma unroll
@@ -359,9 +375,9 @@ __global__ __launch_bounds__(kThreads, 1) void grad_queries_kernel(GradArgs a) {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float p = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -st.x));
+          float p = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -lse));
           if (!whole && !mine.sees(place * kTile + 32 * kb + 16 * c + 8 * g + e)) p = 0.f;
-          x[e] = p * (d[8 * c + e] - st.y);
+          x[e] = p * (d[8 * c + e] - delta);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) df[c][e] = pack2(x[2 * e], x[2 * e + 1]);
@@ -370,13 +386,9 @@ __global__ __launch_bounds__(kThreads, 1) void grad_queries_kernel(GradArgs a) {
       for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
-          dq[db] = mfma32(sK[b].turned(2 * kb + c, db, lane), __builtin_bit_cast(bf16x8, df[c]), dq[db]);
+          dq[db] = mfma32(reader.turned(tk + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, df[c]), dq[db]);
     }
-    if (t + 1 < tiles.n) {
-      lk.put(sK[b ^ 1]);
-      lv.put(sV[b ^ 1]);
-      __syncthreads();
-    }
+    if (t + 1 < tiles.n) arrived();
   }
   if (row >= u.nq) return;
   uint16_t *op = a.dq + (u.q0 + row) * a.dq_token + h * a.dq_head;
