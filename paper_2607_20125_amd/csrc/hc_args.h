@@ -95,6 +95,36 @@ inline void choose_split(SeqArgs &a, int64_t keys, int64_t want, int64_t least, 
   a.n_split = cuts < 2 || !good_grid(units * cuts) ? 1 : (int32_t)cuts;
 }
 
+// 128-dim heads: waves of 64 rows, which run the matrix cores better but start slowly and hide
+// nothing of it (one wave per SIMD), or of 32.  9360 rows of 12 heads (900 work groups) over 256, 512 and
+// 1024 keys: 37, 50 and 75 us against 33, 55 and 95; 1024 rows (96 groups, a
+// part of the card) over 512, 1024 and 2048 keys: 20, 27 and 34 us against 18, 25 and 36.
+inline bool wide_rows(const SeqArgs &a, int64_t keys) {
+  return keys >= ((int64_t)a.tiles * a.kv_heads * a.n_split >= 256 ? 384 : 1536);
+}
+
+// Wide kernel, units that take alike (one sequence without a mask, or a window that is shorter than the sequences): two work
+// groups per CU make 512 places for them.  What is left over after whole rounds would run alone, each unit on a place of its
+// own; instead those units are cut so that their pieces fill the places again: 588 units
+// (6200 rows of 12 heads) over 32760 keys without this took as long as 1024 would.
+inline void cut_last_round(SeqArgs &a, int64_t keys, bool alike) {
+  constexpr int64_t places = 512;
+  const int64_t units = seq_units(a), over = units % places;
+  if (!a.wide || a.n_split != 1 || !alike || units < places || over == 0) return;
+  const int64_t tiles = (keys + kSeqKeys - 1) / kSeqKeys;
+  // rounds of pieces, in units, and what a cut costs: about 8 tiles for the start and end of a
+  // piece and its partial result
+  auto cost = [&](int64_t p) {
+    return (double)((over * p + places - 1) / places) * (1.0 / p + (p > 1 ? 8.0 / tiles : 0.0));
+  };
+  int64_t best = 1;
+  for (int64_t p = 2; p <= 8; ++p)
+    if (cost(p) < cost(best)) best = p;
+  if (best == 1) return;
+  a.whole = (int32_t)(units - over);
+  a.n_split = (int32_t)best;
+}
+
 inline hc_status check_workspace(hc_ctx *c, const void *p, int64_t bytes, int64_t needed) {
   if (needed == 0) return HC_OK;
   if (!p || !aligned16(p) || bytes < needed)

@@ -10,7 +10,8 @@ namespace dev {
 // Keys that a query sees: [0, sink) and [start, end).  All three grow with the query.
 struct Seen {
   int end, sink, start;
-  __device__ __forceinline__ bool sees(int key) const { return key < end && (key < sink || key >= start); }
+  // (without branches: a mask asks for many keys)
+  __device__ __forceinline__ bool sees(int key) const { return (key < end) & ((key < sink) | (key >= start)); }
 };
 // Query i of n over m keys.  (32 bits without a sign hold the end of any position's block.)
 __device__ __forceinline__ Seen seen_of(int block, int window, int sinks, int n, int m, int i) {
@@ -33,15 +34,18 @@ __device__ __forceinline__ Seen seen_by(const SeqArgs &a, const SeqUnit &u, int 
 struct KeyTiles {
   int n;                     // tiles
   int first, gap;            // tiles of the first tokens; tiles left out behind them
-  int lo_end, hi_start;      // of the first and last query
+  int lo_start, lo_end, hi_sink, hi_start, hi_end;      // of the first and last query
   __device__ __forceinline__ KeyTiles(Seen lo, Seen hi) {
     first = (hi.sink + kSeqKeys - 1) / kSeqKeys;
     gap = max(lo.start / kSeqKeys - first, 0);
     n = (hi.end + kSeqKeys - 1) / kSeqKeys;
     if (n <= first + gap) gap = max(n - first, 0);      // (the window begins where the keys end)
     n -= gap;
+    lo_start = lo.start;
     lo_end = lo.end;
+    hi_sink = hi.sink;
     hi_start = hi.start;
+    hi_end = hi.end;
   }
   __device__ __forceinline__ int place(int t) const { return t + (t >= first ? gap : 0); }
   // Whether every row sees all of the tile at this place.

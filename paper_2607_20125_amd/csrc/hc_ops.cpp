@@ -6,36 +6,6 @@ using namespace hc;
 
 namespace {
 
-// 128-dim heads: waves of 64 rows, which run the matrix cores better but start slowly and hide
-// nothing of it (one wave per SIMD), or of 32.  9360 rows of 12 heads (900 work groups) over 256, 512 and
-// 1024 keys: 37, 50 and 75 us against 33, 55 and 95; 1024 rows (96 groups, a
-// part of the card) over 512, 1024 and 2048 keys: 20, 27 and 34 us against 18, 25 and 36.
-bool wide_rows(const SeqArgs &a, int64_t keys) {
-  return keys >= ((int64_t)a.tiles * a.kv_heads * a.n_split >= 256 ? 384 : 1536);
-}
-
-// Wide kernel, one sequence, no mask: all units take alike, and two work groups per CU make 512
-// places for them.  What is left over after whole rounds would run alone, each unit on a place of its
-// own; instead those units are cut so that their pieces fill the places again: 588 units
-// (6200 rows of 12 heads) over 32760 keys without this took as long as 1024 would.
-void cut_last_round(SeqArgs &a, int64_t keys) {
-  constexpr int64_t places = 512;
-  const int64_t units = seq_units(a), over = units % places;
-  if (!a.wide || a.n_split != 1 || a.n_seqs != 1 || a.block != 0 || units < places || over == 0) return;
-  const int64_t tiles = (keys + kSeqKeys - 1) / kSeqKeys;
-  // rounds of pieces, in units, and what a cut costs: about 8 tiles for the start and end of a
-  // piece and its partial result
-  auto cost = [&](int64_t p) {
-    return (double)((over * p + places - 1) / places) * (1.0 / p + (p > 1 ? 8.0 / tiles : 0.0));
-  };
-  int64_t best = 1;
-  for (int64_t p = 2; p <= 8; ++p)
-    if (cost(p) < cost(best)) best = p;
-  if (best == 1) return;
-  a.whole = (int32_t)(units - over);
-  a.n_split = (int32_t)best;
-}
-
 hc_status run_seq(hc_ctx *c, const SeqArgs &a, int head_dim, bool few_rows, hipStream_t s) {
   return timed_launch(c, s, HC_K_SEQUENCE, [&] {
     hipError_t e = few_rows ? launch_decode(a, head_dim, s) : launch_seq(a, head_dim, s);
@@ -84,7 +54,7 @@ hc_status packed_plan(hc_ctx *c, const hc_packed_args *p, SeqArgs &a) {
   // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
   a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24 &&
            wide_rows(a, p->n_keys / p->n_seqs);
-  cut_last_round(a, p->n_keys);
+  cut_last_round(a, p->n_keys, a.n_seqs == 1 && a.block == 0);
   return HC_OK;
 }
 
@@ -175,7 +145,7 @@ hc_status cached_plan(hc_ctx *c, const hc_qcache *k, const hc_qcache_attention_a
   if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units < 192 ? 1024 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);
   a.wide = k->head_dim == 128 && !few_rows && wide_rows(a, keys);
-  cut_last_round(a, keys);
+  cut_last_round(a, keys, a.n_seqs == 1 && a.block == 0);
   return HC_OK;
 }
 

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(SeqArgs a)
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (gone || !mine.sees(place * KT + 32 * c + 8 * g + 4 * kb + r)) s[kb][r] = -INFINITY;
+          if (gone | !mine.sees(place * KT + 32 * c + 8 * g + 4 * kb + r)) s[kb][r] = -INFINITY;
       if (gone)                // any values may stand there: a probability of 0 times 0 is 0
 #pragma unroll
         for (int e = 0; e < 8; ++e)

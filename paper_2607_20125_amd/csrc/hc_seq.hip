@@ -1,6 +1,7 @@
 // Attention over sequences: packed keys and values in bf16, or the 4-bit cache; and
 // the merge of partial results.
 #include "hc_mask.h"
+#include "hc_window.h"
 
 namespace hc {
 namespace {
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = 32 * kb + kperm(8 * (r >> 2) + 4 * g + (r & 3));      // (run key / 16 of the tile)
-            if (!mine.sees(at * KT + key) || (absent_now >> (2 * kb + (r >> 3)) & 1)) s[kb][r] = -INFINITY;
+            if (!mine.sees(at * KT + key) | (absent_now >> (2 * kb + (r >> 3)) & 1)) s[kb][r] = -INFINITY;
           }
       }
     } else if ((t + 1) * KT > lo_all) {
@@ -443,6 +444,7 @@ hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s) {
 }
 
 hipError_t launch_window(const SeqArgs &a, int head_dim, hipStream_t s) {
+  if (head_dim == 128 && a.wide) return launch_window128(a, s);
   const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
   if (head_dim == 128) {
     if (a.table) hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kPaged>), grid, block, 0, s, a);

@@ -1,6 +1,7 @@
 // Attention over sequences for 128-dim heads on waves of 64 rows: packed keys and values
 // in bf16, or the 4-bit cache.
-#include "hc_seq.h"
+#include "hc_mask.h"
+#include "hc_window.h"
 
 namespace hc {
 namespace {
@@ -87,8 +88,9 @@ __device__ __forceinline__ const uint16_t *uniform_ptr(const uint16_t *p) {
   return (const uint16_t *)((uint64_t)hi << 32 | lo);
 }
 
-template <bool QUANT>
-__global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
+template <Keys SRC>
+__device__ __forceinline__ void attend128(const SeqArgs &a) {
+  constexpr bool QUANT = SRC == Keys::kQuant, PAGED = SRC == Keys::kPaged, WINDOW = PAGED || SRC == Keys::kWindow;
   constexpr int D = 128, NQB = 2, KT = kSeqKeys, NKK = D / 16, NDB = D / 32;
   constexpr int TILE = KT * D;               // elements per tile
   constexpr int RK = 2, RV = 3;              // ring buffers
@@ -106,12 +108,20 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
 
   // this lane's rows wave 64 + 32 qb + n of the unit; a row behind the last repeats it
   int hi[NQB];               // keys it sees
+  int start[NQB];            // with a window: those from here on and the first tokens
   bf16x8 qf[NQB][NKK];
 #pragma unroll
   for (int qb = 0; qb < NQB; ++qb) {
     const int at = min(u.row0 + wave * 64 + qb * 32 + n, u.rows - 1);
     const int qi = at / a.group, qh = head * a.group + (at - qi * a.group);
-    hi[qb] = seen_keys(a, u, qi);
+    if constexpr (WINDOW) {
+      const Seen mine = seen_by(a, u, qi);
+      hi[qb] = mine.end;
+      start[qb] = mine.start;
+    } else {
+      hi[qb] = seen_keys(a, u, qi);
+      start[qb] = 0;
+    }
     const uint16_t *qp = a.q + (u.q0 + qi) * a.q_token + qh * a.q_head;
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) qf[qb][kk] = ld_g16(qp + 16 * kk + 8 * g);
@@ -128,14 +138,44 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   // The key range: nt tiles from tile t0 on.  Tiles below `plain` are seen whole by every row
   // (seen_keys grows with the query).
   const int last = min(u.row0 + kSeqRows, u.rows) - 1;
-  const int lo_all = seen_keys(a, u, u.row0 / a.group), hi_all = seen_keys(a, u, last / a.group);
-  const int nt_all = (hi_all + KT - 1) / KT;
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  int lo_all = 0, nt_all;
+  KeyTiles tiles(Seen{}, Seen{});
+  if constexpr (WINDOW) {
+    tiles = KeyTiles(seen_by(a, u, u.row0 / a.group), seen_by(a, u, last / a.group));
+    tiles.first = uniform(tiles.first);
+    tiles.gap = uniform(tiles.gap);
+    tiles.lo_end = uniform(tiles.lo_end);
+    tiles.hi_start = uniform(tiles.hi_start);
+    tiles.lo_start = uniform(tiles.lo_start);
+    tiles.hi_end = uniform(tiles.hi_end);
+    tiles.hi_sink = uniform(tiles.hi_sink);
+    nt_all = tiles.n;
+  } else {
+    lo_all = seen_keys(a, u, u.row0 / a.group);
+    const int hi_all = seen_keys(a, u, last / a.group);
+    nt_all = (hi_all + KT - 1) / KT;
+  }
   int t0, t1;
   key_range(a, u, share, nt_all, t0, t1);
   t0 = __builtin_amdgcn_readfirstlane(t0);
   const int nt = __builtin_amdgcn_readfirstlane(t1 - t0);
   const int plain = __builtin_amdgcn_readfirstlane(lo_all / KT - t0);
-  const int nk = u.nk - t0 * KT;             // keys of the sequence from tile t0 on
+  const int nk = u.nk - (WINDOW ? 0 : t0 * KT);      // keys of the sequence from tile t0 on; with a window, all
+  // Place of the range's tile t: in the sequence with a window, else from tile t0 on; and whether every row sees it whole.
+  auto place = [&](int t) { return WINDOW ? tiles.place(t0 + t) : t; };
+  auto whole = [&](int t) {
+    if constexpr (WINDOW) return tiles.whole(place(t), a.sinks);
+    else return t < plain;
+  };
+  // With a window: the tile behind the run of whole tiles that t is in.
+  auto whole_until = [&](int t) {
+    const int p = place(t);
+    const bool joined = tiles.hi_start <= a.sinks;       // (every key before the first row's end)
+    const int until = joined || p * KT >= tiles.hi_start ? tiles.lo_end / KT - (p >= tiles.first ? tiles.gap : 0)
+                                                         : min(a.sinks, tiles.lo_end) / KT;
+    return until - t0;
+  };
 
   // --- tiles: packed -----------------------------------------------------------------
   // Wave instruction j of a wave fills LDS rows 4 (8 wave + j) .. + 3, 16 chunks each.  K:
@@ -156,21 +196,64 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   };
   auto k_chunk = [&](int j) { return kswz<D>(4 * (8 * wave + j) + dma_row, dma_pos); };
   const int v_chunk = dma_pos ^ (4 * dma_row);
+  const int wave_key = PAGED ? 0 : 32 * wave;       // (pages: rows count from their run of 16)
   if constexpr (!QUANT) {
-    kbase = uniform_ptr(a.k + (u.k0 + (int64_t)t0 * KT) * a.k_token + head * a.k_head);
-    vbase = uniform_ptr(a.v + (u.k0 + (int64_t)t0 * KT) * a.v_token + head * a.v_head);
+    if constexpr (PAGED) {
+      kbase = uniform_ptr(a.k + head * a.k_head);
+      vbase = uniform_ptr(a.v + head * a.v_head);
+    } else {
+      const int64_t from = WINDOW ? 0 : (int64_t)t0 * KT;
+      kbase = uniform_ptr(a.k + (u.k0 + from) * a.k_token + head * a.k_head);
+      vbase = uniform_ptr(a.v + (u.k0 + from) * a.v_token + head * a.v_head);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      ka[j] = (uint32_t)k_key(j) * (uint32_t)a.k_token * 2u + (uint32_t)(k_chunk(j) * 16 + 8192 - 1024 * j);
-    va = (uint32_t)(32 * wave + dma_row) * (uint32_t)a.v_token * 2u + (uint32_t)(v_chunk * 16);
+      ka[j] = (uint32_t)(k_key(j) - 32 * wave + wave_key) * (uint32_t)a.k_token * 2u + (uint32_t)(k_chunk(j) * 16 + 8192 - 1024 * j);
+    va = (uint32_t)(wave_key + dma_row) * (uint32_t)a.v_token * 2u + (uint32_t)(v_chunk * 16);
   }
-  // (instruction 4 half + j)
-  auto dma_k = [&](int t, int half) {
-    lds_dma16_offsets(kbase + ((int64_t)t * KT + 16 * half) * a.k_token - 4096, ka, k_to(t) + 4096 * half);
+  // Pages: where run 2 wave + half of tile t is, by a scalar load.  A run that has no page and that no row sees (its keys are
+  // masked: pages that the window has passed) is read at a run in place of it whose 16 keys all were stored; one that
+  // a row does see is noted.
+  struct Run {
+    int page, run;
   };
-  auto dma_v = [&](int t, int half) {
-    lds_dma16_bases(vbase + ((int64_t)t * KT + 16 * half) * a.v_token, 4 * a.v_token - 512, va,
-                    v_to(t) + 4096 * half);
+  bool gone = false;
+  typedef const int32_t __attribute__((address_space(4))) *sptr;
+  const sptr entries = PAGED ? (sptr)(uintptr_t)(a.table + (int64_t)u.seq * a.table_seq) : sptr();
+  auto entry = [&](int run) { return entries[(run << 4) >> a.page_shift]; };
+  auto present = [&](int p) { return (uint32_t)p < (uint32_t)a.n_pages; };
+  Run stand_in{0, 0};
+  if constexpr (PAGED) {
+    if (nt > 0) {
+      stand_in.run = max(tiles.hi_end / 16 - 1, 0);
+      stand_in.page = entry(stand_in.run);
+      if (!present(stand_in.page)) stand_in = Run{0, 0};
+    }
+  }
+  auto run_in = [&](int t, int half) -> Run {
+    if constexpr (!PAGED) return Run{0, 0};
+    const int run = run_of(u, place(t), 2 * wave + half), p = entry(run);
+    if (present(p)) return Run{p, run};
+    const bool seen = run * 16 < tiles.hi_sink || (run * 16 + 16 > tiles.lo_start && run * 16 < tiles.hi_end);
+    gone = gone || seen || stand_in.run == 0;
+    return stand_in;
+  };
+  // its first row
+  auto run_at = [&](const uint16_t *base, int64_t page_stride, int64_t token, Run r) {
+    return base + r.page * page_stride + run_token(a, r.run) * token;
+  };
+  // (instruction 4 half + j; r: the run in pages)
+  auto dma_k = [&](int t, int half, Run r) {
+    const uint16_t *from;
+    if constexpr (PAGED) from = run_at(kbase, a.k_page, a.k_token, r);
+    else from = kbase + ((int64_t)place(t) * KT + 16 * half) * a.k_token;
+    lds_dma16_offsets(from - 4096, ka, k_to(t) + 4096 * half);
+  };
+  auto dma_v = [&](int t, int half, Run r) {
+    const uint16_t *from;
+    if constexpr (PAGED) from = run_at(vbase, a.v_page, a.v_token, r);
+    else from = vbase + ((int64_t)place(t) * KT + 16 * half) * a.v_token;
+    lds_dma16_bases(from, 4 * a.v_token - 512, va, v_to(t) + 4096 * half);
   };
 
   // --- tiles: 4-bit ---------------------------------------------------------------------
@@ -252,16 +335,27 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       load_k(t);
 #pragma unroll
       for (int i = 0; i < 8; ++i) put_k(k_slot(t), i);
-    } else if ((t + 1) * KT <= nk) {
-      dma_k(t, 0);
-      dma_k(t, 1);
+    } else if ((place(t) + 1) * KT <= nk) {
+      dma_k(t, 0, run_in(t, 0));
+      dma_k(t, 1, run_in(t, 1));
+    } else if constexpr (PAGED) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int run = run_of(u, place(t), 2 * wave + half) * 16 - place(t) * KT;      // its first key, of the tile
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          b[j] = (uint32_t)(min(k_key(4 * half + j), nk - 1 - place(t) * KT) - run) * (uint32_t)a.k_token * 2u +
+                 (uint32_t)(k_chunk(4 * half + j) * 16 + 8192 - 1024 * j);
+        lds_dma16_offsets(run_at(kbase, a.k_page, a.k_token, run_in(t, half)) - 4096, b, k_to(t) + 4096 * half);
+      }
     } else {
       uint32_t b[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        b[j] = (uint32_t)min(k_key(j), nk - 1 - t * KT) * (uint32_t)a.k_token * 2u +
+        b[j] = (uint32_t)min(k_key(j), nk - 1 - place(t) * KT) * (uint32_t)a.k_token * 2u +
                (uint32_t)(k_chunk(j) * 16 + 8192 - 1024 * j);
-      const uint16_t *from = kbase + (int64_t)t * KT * a.k_token - 4096;
+      const uint16_t *from = kbase + (int64_t)place(t) * KT * a.k_token - 4096;
       lds_dma16_offsets(from, b, k_to(t));
       lds_dma16_offsets(from + 2048, b + 4, k_to(t) + 4096);
     }
@@ -272,16 +366,27 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       cut_v(t);
 #pragma unroll
       for (int i = 0; i < 8; ++i) put_v(v_slot(t), i);
-    } else if ((t + 1) * KT <= nk) {
-      dma_v(t, 0);
-      dma_v(t, 1);
+    } else if ((place(t) + 1) * KT <= nk) {
+      dma_v(t, 0, run_in(t, 0));
+      dma_v(t, 1, run_in(t, 1));
+    } else if constexpr (PAGED) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int run = run_of(u, place(t), 2 * wave + half) * 16 - place(t) * KT;
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          b[j] = (uint32_t)(min(4 * (8 * wave + 4 * half + j) + dma_row, nk - 1 - place(t) * KT) - run) * (uint32_t)a.v_token * 2u +
+                 (uint32_t)(v_chunk * 16 + 8192 - 1024 * j);
+        lds_dma16_offsets(run_at(vbase, a.v_page, a.v_token, run_in(t, half)) - 4096, b, v_to(t) + 4096 * half);
+      }
     } else {
       uint32_t b[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        b[j] = (uint32_t)min(4 * (8 * wave + j) + dma_row, nk - 1 - t * KT) * (uint32_t)a.v_token * 2u +
+        b[j] = (uint32_t)min(4 * (8 * wave + j) + dma_row, nk - 1 - place(t) * KT) * (uint32_t)a.v_token * 2u +
                (uint32_t)(v_chunk * 16 + 8192 - 1024 * j);
-      const uint16_t *from = vbase + (int64_t)t * KT * a.v_token - 4096;
+      const uint16_t *from = vbase + (int64_t)place(t) * KT * a.v_token - 4096;
       lds_dma16_offsets(from, b, v_to(t));
       lds_dma16_offsets(from + 2048, b + 4, v_to(t) + 4096);
     }
@@ -351,14 +456,39 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   };
   // keys that a row does not see get no weight
   auto mask = [&](Scores &s, int t) {
+    const int first = (WINDOW ? place(t) : t0 + t) * KT;
+    if (!WINDOW || first + KT > tiles.lo_end) {
 #pragma unroll
-    for (int qb = 0; qb < NQB; ++qb) {
-      const int rem = hi[qb] - (t0 + t) * KT - 8 * g;
+      for (int qb = 0; qb < NQB; ++qb) {
+        const int rem = hi[qb] - first - 8 * g;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)       // (kperm(8 (r / 4) + 4 g + r % 4) = 8 g + kperm(...) at g = 0)
-          if (32 * kb + kperm(8 * (r >> 2) + (r & 3)) >= rem) s[kb][qb][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r)       // (kperm(8 (r / 4) + 4 g + r % 4) = 8 g + kperm(...) at g = 0)
+          {
+            if (32 * kb + kperm(8 * (r >> 2) + (r & 3)) >= rem) s[kb][qb][r] = -INFINITY;
+            if (WINDOW && r % 8 == 7) fence();
+          }
+      }
+    }
+    if constexpr (WINDOW) {
+      // those between the first tokens and the row's window
+      if (first + KT > a.sinks && first < tiles.hi_start) {
+#pragma unroll
+        for (int qb = 0; qb < NQB; ++qb) {
+          int low = first + 8 * g - a.sinks;
+          uint32_t width = (uint32_t)max(start[qb] - a.sinks, 0);
+          asm volatile("" : "+v"(low), "+v"(width));     // (or 32 differences stay in registers for the other rows)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+            {
+              if ((uint32_t)(low + 32 * kb + kperm(8 * (r >> 2) + (r & 3))) < width) s[kb][qb][r] = -INFINITY;
+              if (r % 8 == 7) fence();
+            }
+        }
+      }
     }
   };
   // pair p of a tile's probabilities: key chunk p / 8, row block (p / 4) % 2,
@@ -424,11 +554,20 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
         if (i % 2 == 1) put_v(vn, i / 2);
       slot(i, [&](int qb) { mfma_score(nxt[i % 2][qb], kf[i % 4], qf[qb][i / 2], i < 2); });
     }
+    // (scalar loads come back in any order, so every wait behind one is for all of the LDS reads too: here all are over anyway)
+    Run kr[2] = {}, vr[2] = {};
+    if constexpr (STEADY && PAGED) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        kr[i] = run_in(t + 3, i);
+        vr[i] = run_in(t + 2, i);
+      }
+    }
     if constexpr (!QUANT) wait_vmcnt<0>();     // K(t+2) and V(t+1) landed
     __syncthreads();              // ... for every wave; S(t+1) and PV(t-1) are over
     if constexpr (!STEADY) {
       settle(nxt);
-      if (t + 1 >= plain) mask(nxt, t + 1);
+      if (!whole(t + 1)) mask(nxt, t + 1);
       if constexpr (QUANT) {
         // (K(t+3) is in its registers if it exists)
         if (t + 3 < nt) {
@@ -452,8 +591,8 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       if constexpr (STEADY && QUANT) {
         if (i % 2 == 1) put_k(kslot, i / 2);
       } else if constexpr (STEADY) {
-        if (i < 2) dma_k(t + 3, i);
-        else if (i < 4) dma_v(t + 2, i - 2);
+        if (i < 2) dma_k(t + 3, i, kr[i]);
+        else if (i < 4) dma_v(t + 2, i - 2, vr[i - 2]);
       }
       slot(16 + i, [&](int qb) { acc[qb][i % 4] = mfma32(kf[i % 4], probs(pf, i / 4, qb), acc[qb][i % 4]); });
       if (i % 4 == 3) {
@@ -462,6 +601,22 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       }
     }
     if constexpr (STEADY && QUANT) load_k(t + 4);
+  };
+  // Whether a row sum is out of range already (NaN included).
+  auto sums_over = [&](int t) -> bool {
+    bool over = false;
+#pragma unroll
+    for (int qb = 0; qb < NQB; ++qb)
+      over = over || max(__float_as_uint(lacc[qb][0]), __float_as_uint(lacc[qb][1])) >
+                         __builtin_bit_cast(uint32_t, 0x1p96f);
+    over = __any(lane < 16 && over);
+    // the waves agree through the V slot of tile t - 1: read by both, and
+    // refilled only after the next step's barrier
+    int *flag = reinterpret_cast<int *>(&sV[(t - 1) % RV][0]);
+    __syncthreads();
+    if (lane == 0) flag[wave] = over ? 1 : 0;
+    __syncthreads();
+    return (flag[0] | flag[1]) != 0;
   };
   // Returns false as soon as it cannot stand any more: row sums only grow, so one
   // above the bound after kCheckTile tiles (NaN included) stays above it, and the
@@ -476,7 +631,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     Scores sa, sb;
     Probs pf;
     qk(0, sa);
-    if (plain <= 0) mask(sa, 0);
+    if (!whole(0)) mask(sa, 0);
     __syncthreads();              // S(0) is over for every wave
     if (nt > 2) fetch_k(2);
     if constexpr (QUANT) {
@@ -497,44 +652,72 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       pair(p);
     }
     int t = 0;
-    // the written-out steps end before the last four tiles and before the first masked one
-    const int n_steady = min(nt - 4, plain - 1);
-    if (t < n_steady - 1) {
-      // (QUANT: K(2) was written without a barrier behind it, which the step's own one gives)
+    if constexpr (WINDOW) {
+      // Written-out steps, two at a time from an even tile on, for the whole tiles among the first tokens, then for those
+      // of the window (which may be one run); single ones, masked where they have to be, before, between and behind.
+      bool checked = nt < 4 * kCheckTile;
+      auto steady = [&](int n_steady) -> bool {
+        if (t + 1 >= n_steady) return true;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) kf[i] = ldk(TILE * 2, i);
-      for (int stop = nt >= 4 * kCheckTile && n_steady > kCheckTile ? kCheckTile : n_steady;; stop = n_steady) {
-        for (; t + 1 < n_steady && t < stop; t += 2) {   // two steps, so that the score sets swap roles
-          step(std::true_type{}, t, TILE * 2, sa, sb, pf);
-          step(std::true_type{}, t + 1, 0, sb, sa, pf);
+        for (int i = 0; i < kAhead; ++i) kf[i] = ldk(TILE * 2, i);
+        for (;;) {
+          int stop = n_steady;
+          if (!checked) stop = min(stop, max(t + 2, kCheckTile));
+          for (; t + 1 < stop; t += 2) {
+            step(std::true_type{}, t, TILE * 2, sa, sb, pf);
+            step(std::true_type{}, t + 1, 0, sb, sa, pf);
+          }
+          if (t + 1 >= n_steady) return true;
+          if (!checked && t >= kCheckTile) {
+            checked = true;
+            if (sums_over(t)) return false;
+          }
         }
-        if (stop == n_steady) break;
-        bool over = false;
-#pragma unroll
-        for (int qb = 0; qb < NQB; ++qb)
-          over = over || max(__float_as_uint(lacc[qb][0]), __float_as_uint(lacc[qb][1])) >
-                             __builtin_bit_cast(uint32_t, 0x1p96f);
-        over = __any(lane < 16 && over);
-        // the waves agree through the V slot of tile t - 1: read by both, and
-        // refilled only after the next step's barrier
-        int *flag = reinterpret_cast<int *>(&sV[(t - 1) % RV][0]);
-        __syncthreads();
-        if (lane == 0) flag[wave] = over ? 1 : 0;
-        __syncthreads();
-        if ((flag[0] | flag[1]) != 0) return false;
-      }
-    }
-    while (t + 1 < nt) {
-      step(std::false_type{}, t, k_slot(t + 1), sa, sb, pf);
-      ++t;
-      if (t + 1 < nt) {
-        step(std::false_type{}, t, k_slot(t + 1), sb, sa, pf);
+      };
+      auto single = [&] {
+        step(std::false_type{}, t, k_slot(t + 1), sa, sb, pf);
         ++t;
-      } else {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int qb = 0; qb < NQB; ++qb) sa[kb][qb] = sb[kb][qb];
+      };
+      if (!steady(whole(1) ? min(nt - 4, whole_until(1) - 1) : 0)) return false;
+      const int window = max((tiles.hi_start + KT - 1) / KT - tiles.gap - t0, 0);       // its first whole tile
+      const int n_window = min(nt - 4, tiles.lo_end / KT - tiles.gap - t0 - 1);
+      if (window > 0 && window < n_window) {
+        while (t % 2 != 0 || t + 1 < window) single();
+        if (!steady(n_window)) return false;
+      }
+      while (t + 1 < nt) single();
+    } else {
+      // the written-out steps end before the last four tiles and before the first masked one
+      const int n_steady = min(nt - 4, plain - 1);
+      if (t < n_steady - 1) {
+        // (QUANT: K(2) was written without a barrier behind it, which the step's own one gives)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) kf[i] = ldk(TILE * 2, i);
+        for (int stop = nt >= 4 * kCheckTile && n_steady > kCheckTile ? kCheckTile : n_steady;; stop = n_steady) {
+          for (; t + 1 < n_steady && t < stop; t += 2) {   // two steps, so that the score sets swap roles
+            step(std::true_type{}, t, TILE * 2, sa, sb, pf);
+            step(std::true_type{}, t + 1, 0, sb, sa, pf);
+          }
+          if (stop == n_steady) break;
+          if (sums_over(t)) return false;
+        }
+      }
+      while (t + 1 < nt) {
+        step(std::false_type{}, t, k_slot(t + 1), sa, sb, pf);
+        ++t;
+        if (t + 1 < nt) {
+          step(std::false_type{}, t, k_slot(t + 1), sb, sa, pf);
+          ++t;
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int qb = 0; qb < NQB; ++qb) sa[kb][qb] = sb[kb][qb];
+        }
       }
     }
     // last tile: the rest of its probabilities, PV(nt - 1)
@@ -569,18 +752,40 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
       l_run[qb] = 0.f;
     }
     __syncthreads();              // every wave is done with the slots
+    // (an absent run's rows are copied from page 0 and do not count)
     fetch_k(0);
     fetch_v(0);
     for (int t = 0; t < nt; ++t) {
       arrived();                  // tile t is there, and tile t - 1 is over
+      uint32_t hidden = 0;        // runs
+      if constexpr (PAGED) hidden = absent_runs(a, page_entry(a, u, place(t), lane));
       if (t + 1 < nt) {
         fetch_k(t + 1);
         fetch_v(t + 1);
       }
+      if constexpr (PAGED) {
+        if (hidden) {             // a probability of 0 times 0 is 0
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (hidden >> (i / 2) & 1)
+              *reinterpret_cast<u32x4 *>(&sV[t % RV][i * 1024 + tid * 8]) = u32x4{0, 0, 0, 0};
+          __syncthreads();
+        }
+      }
       Scores s;
       Probs pf;
       qk(t, s);
-      if (t >= plain) mask(s, t);
+      if (!whole(t)) mask(s, t);
+      if constexpr (PAGED) {
+        if (hidden)
+#pragma unroll
+          for (int qb = 0; qb < NQB; ++qb)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (hidden >> (2 * kb + (r >> 3)) & 1) s[kb][qb][r] = -INFINITY;
+      }
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
         float m = -INFINITY;
@@ -632,7 +837,7 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
     if (any_fallback) {
       wait_vmcnt<0>();            // nothing of the abandoned pass is in flight
     } else {
-      bool bad = false;
+      bool bad = gone;
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
         const float s0 = __shfl(lacc[qb][0], n & 15), s1 = __shfl(lacc[qb][1], n & 15);
@@ -642,7 +847,16 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r) amax = max(amax, abs_bits(acc[qb][db][r]));
-        const bool empty = hi[qb] <= t0 * KT;
+        bool empty = hi[qb] <= t0 * KT;
+        if constexpr (WINDOW) {
+          // keys of the range: those of its tiles before and behind the gap
+          const int a0 = min(t0, tiles.first) * KT, a1 = min(t0 + nt, tiles.first) * KT;
+          const int b0 = (max(t0, tiles.first) + tiles.gap) * KT, b1 = (max(t0 + nt, tiles.first) + tiles.gap) * KT;
+          auto meets = [&](int x0, int x1) {
+            return (x0 < min(x1, min(min(a.sinks, start[qb]), hi[qb]))) || max(x0, start[qb]) < min(x1, hi[qb]);
+          };
+          empty = !meets(a0, a1) && !meets(b0, b1);
+        }
         bad = bad || !(fixed_offset_ok(l_run[qb], amax) || (empty && __float_as_uint(l_run[qb]) == 0 && amax == 0));
       }
       bad = __any(bad);
@@ -672,6 +886,13 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
           out.put(n, 8 * db + 2 * rq + g, acc[qb][db][4 * rq] * inv, acc[qb][db][4 * rq + 1] * inv,
                   acc[qb][db][4 * rq + 2] * inv, acc[qb][db][4 * rq + 3] * inv);
       out.store(a, u, head, wave * 64 + qb * 32, lane);
+      if constexpr (WINDOW) {
+        const int row = u.row0 + lrow;
+        if (a.lse && g == 0 && row < u.rows) {
+          const int qi = row / a.group, qh = head * a.group + (row - qi * a.group);
+          a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run[qb], l_tot);
+        }
+      }
     } else {
       float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
       float *op = pp + (int64_t)lrow * D;
@@ -689,12 +910,29 @@ __global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
   }
 }
 
+template <bool QUANT>
+__global__ __launch_bounds__(128, 1) void seq_attn128_kernel(SeqArgs a) {
+  attend128<QUANT ? Keys::kQuant : Keys::kPacked>(a);
+}
+// With a window: packed tensors, or pages.
+template <bool PAGED>
+__global__ __launch_bounds__(128, 1) void window_attn128_kernel(SeqArgs a) {
+  attend128<PAGED ? Keys::kPaged : Keys::kWindow>(a);
+}
+
 }  // namespace
 
 hipError_t launch_seq128(const SeqArgs &a, hipStream_t s) {
   const dim3 grid((uint32_t)seq_groups(a)), block(128);
   if (a.cache) hipLaunchKernelGGL((seq_attn128_kernel<true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((seq_attn128_kernel<false>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window128(const SeqArgs &a, hipStream_t s) {
+  const dim3 grid((uint32_t)seq_groups(a)), block(128);
+  if (a.table) hipLaunchKernelGGL((window_attn128_kernel<true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((window_attn128_kernel<false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

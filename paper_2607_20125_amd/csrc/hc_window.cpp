@@ -174,6 +174,9 @@ hc_status paged_plan(hc_ctx *c, const hc_pages *pages, const hc_page_table *tabl
   const int64_t units = seq_units(a);
   if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units < 192 ? 1024 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);
+  // (the wide kernel's copies hold offsets of a run of 16 rows in 32 bits)
+  a.wide = pages->head_dim == 128 && !few_rows && a.k_token < 1 << 24 && a.v_token < 1 << 24 && wide_rows(a, keys);
+  cut_last_round(a, keys, a.window > 0 || (a.n_seqs == 1 && a.block == 0));
   return HC_OK;
 }
 
@@ -214,6 +217,10 @@ hc_status window_plan(hc_ctx *c, const hc_window_args *p, SeqArgs &a) {
   // of several, which ends last, is taken for twice the average)
   const int64_t keys = (int64_t)p->n_keys / p->n_seqs * (p->cu_q && p->n_seqs > 1 ? 2 : 1);
   choose_split(a, seen_at_most(a, keys, kSeqRows), 512, 8, kSeqMaxSplit);
+  // (the wide kernel's copies hold offsets of 63 rows in 32 bits)
+  a.wide = p->head_dim == 128 && p->k_token < 1 << 24 && p->v_token < 1 << 24 &&
+           wide_rows(a, seen_at_most(a, p->n_keys / p->n_seqs, kSeqRows));
+  cut_last_round(a, seen_at_most(a, keys, kSeqRows), a.window > 0 || (a.n_seqs == 1 && a.block == 0));
   return HC_OK;
 }
 
@@ -459,6 +466,9 @@ hc_status hc_window_attention_backward(hc_ctx *c, const hc_window_grad_args *g, 
     if (st == HC_OK) st = check_output(c, {"dv", g->dv, g->dv_token, g->dv_head, p.n_keys, p.n_kv_heads}, p.head_dim);
   }
   if (st != HC_OK) return st;
+  // (the copies of 64 rows hold their offsets in 32 bits)
+  for (int64_t stride : {p.n_tokens > 1 ? std::max(p.q_token, g->dout_token) : 0, p.n_keys > 1 ? std::max(p.k_token, p.v_token) : 0})
+    if (stride >= 1 << 24) return fail(c, HC_E_INVAL, "token strides must be below 2^24");
   if ((st = check_workspace(c, g->workspace, g->workspace_bytes, grad_bytes(p, a))) != HC_OK) return st;
   a.stats = (float *)g->workspace;
   a.part = (float *)((char *)g->workspace + grad_stat_bytes(p));

@@ -1,5 +1,5 @@
 // Internal structures of the operators of a model with a sliding window (hc_window.cpp, hc_norm.hip,
-// hc_paged.hip, hc_window.hip, hc_window128.hip, hc_window_grad.hip).  Not part of the public ABI.
+// hc_paged.hip, hc_window_grad.hip, and the kernels of hc_seq.hip and hc_seq128.hip).  Not part of the public ABI.
 #pragma once
 
 #include "hc_ops.h"
@@ -43,9 +43,9 @@ struct PagedRowsArgs {
 hipError_t launch_paged_append(const PagedRowsArgs &a, hipStream_t s);
 
 // --- attention with a window ------------------------------------------------------------
-// SeqArgs with `windowed`; the sources are hc_window.hip (waves of 32 rows), hc_window128.hip (of 64) and
-// hc_paged.hip (few rows).
+// By waves of 32 rows (hc_seq.hip) or of 64 (hc_seq128.hip), and for few rows (hc_paged.hip).
 hipError_t launch_window(const SeqArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_window128(const SeqArgs &a, hipStream_t s);
 hipError_t launch_paged_decode(const SeqArgs &a, int head_dim, hipStream_t s);
 
 // Gradients.  Rows and units are those of the forward pass; key units are runs of kGradKeys keys of a sequence.

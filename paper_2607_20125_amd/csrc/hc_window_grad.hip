@@ -62,6 +62,54 @@ struct Reader {
   }
 };
 
+// N DMA instructions (see hc_device.h) behind a wait that covers a base which a vector instruction put into its scalar
+// registers just before: 5 wait states, which the compiler does not count for inline assembly.
+template <int N>
+__device__ __forceinline__ void lds_dma16_settled(const uint16_t *base, const uint32_t (&a)[N], uint32_t lds) {
+  static_assert(N == 2 || N == 4, "instructions");
+  uint32_t saved;
+  if constexpr (N == 2) {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %4\n\t"
+        "s_nop 4\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(a[0]), "v"(a[1]), "s"(base), "s"(lds)
+        : "memory");
+  } else {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %6\n\t"
+        "s_nop 4\n\t"
+        "global_load_lds_dwordx4 %1, %5\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base), "s"(lds)
+        : "memory");
+  }
+}
+
+// 64 words to LDS by DMA, word i of the `left` behind p (the last repeats) to place i.
+__device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uint32_t lds) {
+  uint32_t saved;
+  const uint32_t at = (uint32_t)min(lane, left - 1) * 4u;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 4\n\t"
+      "global_load_lds_dword %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(at), "s"(p), "s"(lds)
+      : "memory");
+}
+
 // Copies a tile to LDS by DMA: rows first .. first + 63 (those behind the last repeat it) of one head.  Instruction j
 // of wave w moves 1 KB, the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its
 // 16 bytes.  (The base is 4 KB low, so that no offset goes below zero when 1024 j is taken off.)
@@ -79,7 +127,7 @@ struct Copier {
     for (int j = 0; j < N; ++j)
       a[j] = (uint32_t)min(row + j * RW, left - 1) * (uint32_t)token * 2u +
              (uint32_t)(tswz<D>(row + j * RW, l % (D / 8)) * 16 + 4096 - 1024 * j);
-    lds_dma16_run<N>(p - 2048, a, lds_addr(tile + wave * N * 512));
+    lds_dma16_settled<N>(p - 2048, a, lds_addr(tile + wave * N * 512));
   }
 };
 
@@ -110,21 +158,6 @@ __global__ __launch_bounds__(256) void grad_stats_kernel(GradArgs a) {
     a.stats[at] = a.lse[at] * 1.4426950408889634f;
     a.stats[(int64_t)heads * a.seq.n_tokens + at] = sum;
   }
-}
-
-// 64 words to LDS by DMA, word i of the `left` behind p (the last repeats) to place i.
-__device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uint32_t lds) {
-  uint32_t saved;
-  const uint32_t at = (uint32_t)min(lane, left - 1) * 4u;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\t"
-      "s_mov_b32 m0, %3\n\t"
-      "s_nop 4\n\t"
-      "global_load_lds_dword %1, %2\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(at), "s"(p), "s"(lds)
-      : "memory");
 }
 
 // P and dS of 8 rows as matrix operands
@@ -227,7 +260,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_keys_kernel(GradArgs a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int i = r0 + at + e;
-              if (i < lo || i >= hi) p[e] = 0.f;
+              if ((i < lo) | (i >= hi)) p[e] = 0.f;
             }
 #pragma unroll
           for (int e = 0; e < 8; ++e) d[e] = p[e] * (t[8 * c + e] - sR[b][1][at + e]);
@@ -375,10 +408,13 @@ __global__ __launch_bounds__(kThreads, 2) void grad_queries_kernel(GradArgs a) {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float p = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -lse));
-          if (!whole && !mine.sees(place * kTile + 32 * kb + 16 * c + 8 * g + e)) p = 0.f;
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -lse));
           x[e] = p * (d[8 * c + e] - delta);
         }
+        if (!whole)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!mine.sees(place * kTile + 32 * kb + 16 * c + 8 * g + e)) x[e] = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) df[c][e] = pack2(x[2 * e], x[2 * e + 1]);
       }

@@ -374,3 +374,89 @@ def test_together(ctx):
             if p * page >= sinks and (p + 1) * page <= at + 1 - window and int(table[0, p]) >= 0:
                 pages.k[int(table[0, p])] = math.nan
                 table[0, p] = -1
+
+
+# --- the kernels for long key ranges ---------------------------------------------------------------
+
+LONG = [
+    # kv heads, group, queries, keys, page
+    (2, 1, [1700], None, 64),
+    (1, 4, [130, 500], [2100, 1900], 16),
+    (12, 1, [2600], None, 256),                  # 252 units
+    (1, 2, [300, 1], [1600, 3000], 32),
+]
+LONG_MASKS = [(0, 0, 0), (1, 0, 0), (1, 700, 0), (1, 1000, 130), (1, 64, 1300), (300, 600, 300), (128, 512, 64), (500, 500, 0), (1, 1, 900)]
+
+
+@pytest.mark.parametrize("mask", LONG_MASKS, ids=lambda m: "block%d_window%d_sinks%d" % m)
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_long_sequences_of_128_dims(ctx, case, mask):
+    kv_heads, group, queries, keys, page = LONG[case]
+    block, window, sinks = mask
+    lengths, heads, d = keys or queries, kv_heads * group, 128
+    q, k, v = (normal(200 + i, sum(n), h, d) for i, (n, h) in enumerate(((queries, heads), (lengths, kv_heads), (lengths, kv_heads))))
+    kw = dict(causal_block=block, window=window, sinks=sinks)
+    lse = torch.full((heads, sum(queries)), math.nan, device="cuda")
+    packed = ctx.window_attention(spaced(q), spaced(k), spaced(v), offsets(queries), offsets(lengths) if keys else None, lse=lse, **kw)
+    cut = torch.tensor([0] + lengths).cumsum(0).tolist()
+    parts = [[t[cut[s]:cut[s + 1]] for s in range(len(lengths))] for t in (k, v)]
+    pages, table = fill_pages(ctx, *parts, lengths, page, 8)
+    paged = ctx.paged_attention(pages, table, q.cuda(), ints(lengths), offsets(queries), **kw)
+    at = 0
+    for s, (n, m) in enumerate(zip(queries, lengths)):
+        # some heads of the many
+        some = list(range(0, heads, max(1, heads // 3)))
+        for h in some:
+            out, mag, logs, _ = W.attention(q[at:at + n, h:h + 1], parts[0][s][:, h // group:h // group + 1],
+                                            parts[1][s][:, h // group:h // group + 1], W.sees(n, m, block, window, sinks))
+            W.assert_attention(packed[at:at + n, h:h + 1], out, mag, f"packed {s} {h}")
+            W.assert_attention(paged[at:at + n, h:h + 1], out, mag, f"paged {s} {h}")
+            got = lse[h, at:at + n].cpu().double()
+            assert torch.equal(torch.isinf(got), torch.isinf(logs[0]))
+            assert bool((torch.nan_to_num(got - logs[0], nan=0.0).abs() <= 2.0 ** -8 * 1.02).all())
+        at += n
+
+
+@pytest.mark.parametrize("mask", [(1, 0, 0), (1, 1000, 130), (300, 600, 300)], ids=lambda m: "block%d_window%d_sinks%d" % m)
+def test_long_sequences_with_large_logits_and_absent_pages(ctx, mask):
+    """Units whose fixed softmax offset does not stand run again with a running maximum, and so do those with a page
+    that is gone."""
+    block, window, sinks = mask
+    n, m, d = 400, 2300, 128
+    seen = W.sees(n, m, block, window, sinks)
+    kw = dict(causal_block=block, window=window, sinks=sinks)
+    for spread in (1.0, 40.0):
+        q, k, v = normal(210, n, 4, d, spread=spread), normal(211, m, 4, d, spread=spread), normal(212, m, 4, d)
+        out, mag, _, _ = W.attention(q, k, v, seen)
+        W.assert_attention(ctx.window_attention(q.cuda(), k.cuda(), v.cuda(), None, offsets([m]), **kw), out, mag, "packed")
+        pages, table = fill_pages(ctx, [k], [v], [m], 16, 8)
+        W.assert_attention(ctx.paged_attention(pages, table, q.cuda(), ints([m]), **kw), out, mag, "paged")
+    gone = [(0, p) for p in (0, 3, 70, 121, 143)]
+    pages, table = fill_pages(ctx, [k], [v], [m], 16, 8, gone)
+    for _, p in gone:
+        seen[:, p * 16:(p + 1) * 16] = False
+    out, mag, _, _ = W.attention(q, k, v, seen)
+    W.assert_attention(ctx.paged_attention(pages, table, q.cuda(), ints([m]), **kw), out, mag, "absent")
+
+
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_pages_that_the_window_has_passed(ctx, page):
+    """A chunk whose window begins inside a tile and a page: giving the pages before it away changes no bit."""
+    n, window, sinks, heads = 300, 1000, 40, 2
+    lengths = [2301, 1777, 3010]
+    k, v = ([normal(220 + s + o, m, heads, 128) for s, m in enumerate(lengths)] for o in (0, 10))
+    q = normal(240, 3 * n, 2 * heads, 128).cuda()
+    pages, table = fill_pages(ctx, k, v, lengths, page, 8)
+    kw = dict(causal_block=1, window=window, sinks=sinks)
+    whole = ctx.paged_attention(pages, table, q, ints(lengths), **kw)
+    for s, m in enumerate(lengths):
+        for p in range(-(-m // page)):
+            if p * page >= sinks and (p + 1) * page <= m - n + 1 - window:
+                pages.k[int(table[s, p])] = math.nan
+                pages.v[int(table[s, p])] = math.nan
+                table[s, p] = -1
+    assert int((table < 0).sum()) > 3 * 900 // page
+    assert torch.equal(ctx.paged_attention(pages, table, q, ints(lengths), **kw), whole)
+    for s, m in enumerate(lengths):
+        out, mag, _, _ = W.attention(q[s * n:(s + 1) * n].cpu(), k[s], v[s], W.sees(n, m, 1, window, sinks))
+        W.assert_attention(whole[s * n:(s + 1) * n], out, mag, f"sequence {s}")
