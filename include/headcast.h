@@ -562,7 +562,8 @@ hc_status hc_window_attention(hc_ctx *ctx, const hc_window_args *args, hc_stream
  * workspace is not used.  With p the probabilities and s the scale,
  *   dv = p^T dout,  ds = p (dout v^T - rowsum(dout out)) s,  dq = ds k,  dk = ds^T q,
  * summed over the query heads that share a key head.  p and ds are rounded to bfloat16 for the products, sums are
- * float32, rounded once; repeated calls agree bit for bit.  Token strides of q, k, v and dout are below 2^24.  Rows outside every sequence are left as they were; a key that
+ * float32, rounded once; repeated calls agree bit for bit.  Token strides of q, k, v and dout are below 2^24, a given
+ * softmax_scale not below 2^-100.  Rows outside every sequence are left as they were; a key that
  * no query sees gets zeros.  Async. */
 typedef struct {
   hc_window_args forward;

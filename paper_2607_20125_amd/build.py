@@ -54,7 +54,7 @@ def build_library(verbose: bool = False) -> str:
 
     with tempfile.TemporaryDirectory(prefix="headcast_build_") as tdir:
         objs = [os.path.join(tdir, src + ".o") for src in SOURCES]
-        cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip") else vgpr_form)
+        cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip", "hc_window_grad.hip") else vgpr_form)
                 + (routed if src in ROUTED else [])
                 + ["-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
         with concurrent.futures.ThreadPoolExecutor(max_workers=len(cmds)) as ex:

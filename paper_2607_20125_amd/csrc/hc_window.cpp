@@ -466,6 +466,8 @@ hc_status hc_window_attention_backward(hc_ctx *c, const hc_window_grad_args *g, 
     if (st == HC_OK) st = check_output(c, {"dv", g->dv, g->dv_token, g->dv_head, p.n_keys, p.n_kv_heads}, p.head_dim);
   }
   if (st != HC_OK) return st;
+  // (logarithms of the rows' sums are divided by it)
+  if (a.scale < 0x1p-100f) return fail(c, HC_E_INVAL, "softmax_scale must not be below 2^-100");
   // (the copies of 64 rows hold their offsets in 32 bits)
   for (int64_t stride : {p.n_tokens > 1 ? std::max(p.q_token, g->dout_token) : 0, p.n_keys > 1 ? std::max(p.k_token, p.v_token) : 0})
     if (stride >= 1 << 24) return fail(c, HC_E_INVAL, "token strides must be below 2^24");

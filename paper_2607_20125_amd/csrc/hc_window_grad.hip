@@ -29,15 +29,36 @@ __device__ __forceinline__ int tswz(int r, int c) {
   return c ^ (D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3));
 }
 
-// Streamed tiles in LDS: two of each of two tensors.  Addresses are a lane's own part, and constants.
+// Streamed tiles in LDS: a ring of them, two tensors each.  Addresses are a lane's own part, and constants.
+constexpr int kRing = 4;
+// Operands of a step are read some products ahead: each feeds one product of 32 cycles, and a read takes longer than four.  (So
+// many that the ring of them comes around with every step.)
+constexpr int operands_ahead(int products) { return products % 8 == 0 ? 7 : 5; }
 template <int D>
 struct Streamed {
-  static constexpr int BYTES = kTile * D * 2;
-  uint16_t x[2][2][kTile * D];         // [buffer][tensor]
+  static constexpr int BYTES = kTile * D * 2, SLOT = 2 * BYTES;
+  uint16_t x[kRing][2][kTile * D];
 };
 using lds8 = const __attribute__((address_space(3))) bf16x8 *;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 using ldst = __attribute__((address_space(3))) s16x4 *;
+using ldsf4 = const __attribute__((address_space(3))) f32x4 *;
+// The products S and T, with their stationary operand in the accumulation registers.  (Inline assembly: as the compiler
+// places it, that operand is copied for every product.  tests/test_window_code.py looks at the distance between these products
+// and what reads them.)
+__device__ __forceinline__ void mfma_first(f32x16 &c, bf16x8 a, const bf16x8 &b) {
+  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
+}
+__device__ __forceinline__ void mfma_first(f32x16 &c, bf16x8 a, const bf16x8 &b, const f32x16 &from) {
+  // (a product reads what a vector instruction wrote 2 wait states before at the earliest: `from` may be a copy)
+  asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(c) : "v"(a), "a"(b), "v"(from));
+}
+__device__ __forceinline__ void mfma_first_zero(f32x16 &c, bf16x8 a, const bf16x8 &b) {
+  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
+}
+// Matrix results in their registers before vector instructions use them: a 32x32x16 product needs at most 18 wait states.
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3"); }
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int D>
 struct Reader {
@@ -49,48 +70,50 @@ struct Reader {
     turn = (uint32_t)(r * D * 2 + tswz<D>(r, chunk) * 16 + (i % 2) * 8);
     turn4 = (uint32_t)((r + 4) * D * 2 + tswz<D>(r + 4, chunk) * 16 + (i % 2) * 8);
   }
-  // A operand of a score product: 16 dims kk of rows kperm(n) of the 32 at `tile`
-  __device__ __forceinline__ bf16x8 score(uint32_t tile, int kk) const {
-    return *(lds8)(uintptr_t)((row ^ (uint32_t)(32 * kk)) + tile);
+  // Operand i of a block's first products, whose tile is at `at` + row: dims 16 (i / 2) of its 32 rows, of tensor i % 2.
+  static __device__ __forceinline__ bf16x8 first(uint32_t at, int i) {
+    return *(lds8)(uintptr_t)((at ^ (uint32_t)(32 * (i / 2))) + (uint32_t)(i % 2 * Streamed<D>::BYTES));
   }
-  // A operand of a second product: dims 32 db .. + 31 of the 16 rows at `tile`
-  __device__ __forceinline__ bf16x8 turned(uint32_t tile, int db) const {
+  // Operand of its second products, `at` and `at4` + turn and turn4: dims 32 db .. of rows 16 c .., transposed.
+  static __device__ __forceinline__ bf16x8 second(uint32_t at, uint32_t at4, int tensor, int c, int db) {
+    const uint32_t off = (uint32_t)(tensor * Streamed<D>::BYTES + c * 16 * D * 2), x = (uint32_t)(64 * db);
     struct { s16x4 a, b; } w;
-    w.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((turn ^ (uint32_t)(64 * db)) + tile));
-    w.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((turn4 ^ (uint32_t)(64 * db)) + tile));
+    w.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((at ^ x) + off));
+    w.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ldst)(uintptr_t)((at4 ^ x) + off));
     return __builtin_bit_cast(bf16x8, w);
   }
 };
 
-// N DMA instructions (see hc_device.h) behind a wait that covers a base which a vector instruction put into its scalar
-// registers just before: 5 wait states, which the compiler does not count for inline assembly.
+// N DMA instructions (see hc_device.h), instruction j from base[j] + a[j] (bytes), behind a wait that covers a base which a
+// vector instruction put into its scalar registers just before: 5 wait states, which the compiler does not count for
+// inline assembly.  (base[j] is 1024 j low: the offset counts at both ends.)
 template <int N>
-__device__ __forceinline__ void lds_dma16_settled(const uint16_t *base, const uint32_t (&a)[N], uint32_t lds) {
+__device__ __forceinline__ void lds_dma16_each(const uint16_t *const (&base)[N], const uint32_t (&a)[N], uint32_t lds) {
   static_assert(N == 2 || N == 4, "instructions");
   uint32_t saved;
   if constexpr (N == 2) {
     asm volatile(
         "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %4\n\t"
+        "s_mov_b32 m0, %5\n\t"
         "s_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %2, %4 offset:0x400\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "s"(base), "s"(lds)
+        : "v"(a[0]), "v"(a[1]), "s"(base[0]), "s"(base[1]), "s"(lds)
         : "memory");
   } else {
     asm volatile(
         "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %6\n\t"
+        "s_mov_b32 m0, %9\n\t"
         "s_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
+        "global_load_lds_dwordx4 %2, %6 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %3, %7 offset:0x800\n\t"
+        "global_load_lds_dwordx4 %4, %8 offset:0xc00\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base), "s"(lds)
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]), "s"(lds)
         : "memory");
   }
 }
@@ -110,28 +133,41 @@ __device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uin
       : "memory");
 }
 
-// Copies a tile to LDS by DMA: rows first .. first + 63 (those behind the last repeat it) of one head.  Instruction j
-// of wave w moves 1 KB, the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its
-// 16 bytes.  (The base is 4 KB low, so that no offset goes below zero when 1024 j is taken off.)
+// Copies a tile to LDS by DMA: 64 rows of one head (those behind the last repeat it).  Instruction j of wave w moves 1 KB,
+// the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its 16 bytes.
 template <int D>
 struct Copier {
   static constexpr int RW = 512 / D, N = kTile / RW / kWaves;     // rows of an instruction, instructions of a wave
   int lane, wave;
-  // p: the tile's first row; left: rows from there on.  (A row's offset stays below 2^31: token strides are below 2^24.)
-  __device__ __forceinline__ void copy(const uint16_t *p, int64_t token, int left, uint16_t *tile) const {
-    int l = lane;
-    asm volatile("" : "+v"(l));      // (the rest is computed at each copy: kept in registers it makes others spill)
-    const int row = N * wave * RW + l / (D / 8);
-    uint32_t a[N];
+  uint32_t chunk[N];         // byte of a row that goes to this lane's place
+  __device__ __forceinline__ Copier(int l, int w) : lane(l), wave(w) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      a[j] = (uint32_t)min(row + j * RW, left - 1) * (uint32_t)token * 2u +
-             (uint32_t)(tswz<D>(row + j * RW, l % (D / 8)) * 16 + 4096 - 1024 * j);
-    lds_dma16_settled<N>(p - 2048, a, lds_addr(tile + wave * N * 512));
+    for (int j = 0; j < N; ++j) chunk[j] = (uint32_t)(tswz<D>(N * w * RW + l / (D / 8) + j * RW, l % (D / 8)) * 16);
+  }
+  // p: the tile's first row; left: rows from there on.  (A row's offset stays below 2^31: token strides are below 2^24.)
+  __device__ __forceinline__ void copy(const uint16_t *p, int64_t token, int left, uint32_t tile) const {
+    uint32_t a[N];
+    const uint16_t *base[N];
+    const int row = lane / (D / 8);
+    if (left >= kTile) {
+      const uint32_t off = (uint32_t)row * (uint32_t)token * 2u;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        a[j] = chunk[j] + off;
+        base[j] = p + (int64_t)((N * wave + j) * RW) * token - 512 * j;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        a[j] = chunk[j] + (uint32_t)min((N * wave + j) * RW + row, left - 1) * (uint32_t)token * 2u;
+        base[j] = p - 512 * j;
+      }
+    }
+    lds_dma16_each<N>(base, a, tile + (uint32_t)(wave * N * 1024));
   }
 };
 
-// --- rowsum(dO O), and the logarithms in log2 units -------------------------------------------------
+// --- rowsum(dO O), and the logarithms in units of products of dims -------------------------------------------------
 // A thread takes 8 dims of a row of a head; the 8 or 16 threads of a row add up.
 template <int D>
 __global__ __launch_bounds__(256) void grad_stats_kernel(GradArgs a) {
@@ -155,8 +191,9 @@ __global__ __launch_bounds__(256) void grad_stats_kernel(GradArgs a) {
   for (int d = 1; d < C; d *= 2) sum += __shfl_xor(sum, d);
   if (live && c == 0) {
     const int64_t at = (int64_t)h * a.seq.n_tokens + row;
-    a.stats[at] = a.lse[at] * 1.4426950408889634f;
-    a.stats[(int64_t)heads * a.seq.n_tokens + at] = sum;
+    // (where a product over dims begins from them, it ends as the logit less the logarithm, and as dP - rowsum)
+    a.stats[at] = -a.lse[at] / a.scale;
+    a.stats[(int64_t)heads * a.seq.n_tokens + at] = -sum;
   }
 }
 
@@ -168,10 +205,10 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 
 // --- dK and dV: a work group takes 128 keys of a key head, each wave 32 --------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void grad_keys_kernel(GradArgs a) {
+__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(GradArgs a) {
   constexpr int NKK = D / 16, NDB = D / 32;
   __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // queries, output gradients
-  __shared__ __attribute__((aligned(1024))) float sR[2][2][kTile]; // logarithms, rowsum(dO O)
+  __shared__ __attribute__((aligned(1024))) float sR[kRing][2][kTile];      // their logarithms, rowsum(dO O)
   const SeqArgs &q = a.seq;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
@@ -209,77 +246,142 @@ __global__ __launch_bounds__(kThreads, 2) void grad_keys_kernel(GradArgs a) {
       kf[kk] = ld_g16(kp + 16 * kk);
       vf[kk] = ld_g16(vp + 16 * kk);
     }
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(kf[kk]), "+a"(vf[kk]));
   }
   f32x16 dk[NDB], dv[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = f32x16{};
 
-  const Copier<D> copier{lane, wave};
-  const Reader<D> reader(lane);
+  const Copier<D> copier(lane, wave);
+  using R = Reader<D>;
+  const R reader(lane);
   const int64_t plane = (int64_t)q.n_tokens * q.kv_heads * q.group;
-  auto load = [&](int item, int b) {
+  const uint32_t tiles = lds_addr(&sT), rows = lds_addr(&sR);
+  auto slot = [&](int item) { return (uint32_t)((item - i0) % kRing); };
+  // (every wave copies one run of the rows' numbers, so that all have as many copies in flight; two waves copy the same)
+  auto load = [&](int item) {
     const int h = head * q.group + item / nt, r0 = first + item % nt * kTile;
-    copier.copy(q.q + (u.q0 + r0) * q.q_token + h * q.q_head, q.q_token, u.nq - r0, sT.x[b][0]);
-    copier.copy(a.dout + (u.q0 + r0) * a.do_token + h * a.do_head, a.do_token, u.nq - r0, sT.x[b][1]);
-    if (wave < 2)
-      lds_dma4(a.stats + wave * plane + (int64_t)h * q.n_tokens + u.q0 + r0, u.nq - r0, lane, lds_addr(sR[b][wave]));
+    const uint32_t to = tiles + slot(item) * Streamed<D>::SLOT;
+    copier.copy(q.q + (u.q0 + r0) * q.q_token + h * q.q_head, q.q_token, u.nq - r0, to);
+    copier.copy(a.dout + (u.q0 + r0) * a.do_token + h * a.do_head, a.do_token, u.nq - r0, to + Streamed<D>::BYTES);
+    lds_dma4(a.stats + wave % 2 * plane + (int64_t)h * q.n_tokens + u.q0 + r0, u.nq - r0, lane,
+             rows + slot(item) * 512 + wave % 2 * 256);
   };
-  // what this wave has in flight has arrived, and then what every wave had
-  auto arrived = [&] {
-    wait_vmcnt<0>();
-    __syncthreads();
+  constexpr int COPIES = 2 * Copier<D>::N + 1;           // of a wave and tile
+
+  // A step is block b of 32 rows: beside the products S and T of block b + 1 go the exponentials of block b, then
+  // its products dV and dK.  Operands are read AHEAD products ahead.
+  struct Scores {
+    f32x16 s, t;
+  };
+  constexpr int NF = 2 * NKK, NS = 4 * NDB, EACH = 16 / NF;      // products of each half; exponentials beside one
+  constexpr int AHEAD = operands_ahead(NF + NS), RO = AHEAD + 1;
+  static_assert((NF + NS) % RO == 0, "the ring of operands");
+  bf16x8 op[RO];
+  const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
+  auto read_first = [&](uint32_t at, int i) { return R::first(at, i); };
+  auto read_second = [&](uint32_t at, uint32_t at4, int j) {       // dV from the output gradients, dK from the queries
+    return R::second(at, at4, 1 - j % 2, j / (2 * NDB), j / 2 % NDB);
+  };
+  // Where block qb of an item's tile is, and its rows' numbers.
+  auto block_at = [&](int item, int qb) { return tiles + slot(item) * Streamed<D>::SLOT + (uint32_t)(qb * 32 * D * 2); };
+  auto begin = [&](Scores &x, int item, int qb, int i) {         // rows 4 i .. of a lane's 16
+    const uint32_t at = rows + slot(item) * 512 + (uint32_t)(qb * 128 + g * 32);
+    const f32x4 l = *(ldsf4)(uintptr_t)(at + (uint32_t)(i / 2 * 64 + i % 2 * 16));
+    const f32x4 d = *(ldsf4)(uintptr_t)(at + (uint32_t)(256 + i / 2 * 64 + i % 2 * 16));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x.s[4 * i + e] = l[e];
+      x.t[4 * i + e] = d[e];
+    }
+  };
+  // rows that do not see this lane's key get no weight
+  auto mask = [&](Scores &x, int row) {
+    const uint32_t from = (uint32_t)(row + 8 * g - lo), width = (uint32_t)(hi - lo);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (from + (uint32_t)(16 * (e / 8) + e % 8) >= width) x.s[e] = -INFINITY;
+  };
+  auto step = [&](Scores &cur, Scores &nxt, int item, int qb) {
+    const int item1 = item + qb;                         // of block b + 1
+    const uint32_t next = block_at(item1, 1 - qb) + lane_row, after = block_at(item + 1, qb) + lane_row;
+    const uint32_t here = block_at(item, qb) + turn, here4 = block_at(item, qb) + turn4;
+    auto read_ahead = [&](int i) {
+      const int r = i + AHEAD;
+      op[r % RO] = r < NF ? read_first(next, r) : r < NF + NS ? read_second(here, here4, r - NF) : read_first(after, r - NF - NS);
+    };
+    u32x4 pf[2], df[2];
+    float p0 = 0.f, d0 = 0.f, last = 0.f;
+    // what is left of an element once its exponential is there
+    auto rest = [&](int e, float p) {
+      const float d = p * cur.t[e];
+      if (e % 2 == 0) {
+        p0 = p;
+        d0 = d;
+      } else {
+        pf[e / 8][e % 8 / 2] = pack2(p0, p);
+        df[e / 8][e % 8 / 2] = pack2(d0, d);
+      }
+    };
+    fence();
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      read_ahead(i);
+      mfma_first(i % 2 == 0 ? nxt.s : nxt.t, op[i % RO], i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
+      fence();
+#pragma unroll
+      for (int e = EACH * i; e < EACH * (i + 1); ++e) {
+        const float p = __builtin_amdgcn_exp2f(cur.s[e] * q.scale_log2);
+        if (e > 0) rest(e - 1, last);
+        last = p;
+      }
+      fence();
+    }
+    rest(15, last);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      read_ahead(NF + j);
+      const int c = j / (2 * NDB), db = j / 2 % NDB;
+      if (j % 2 == 0) dv[db] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, pf[c]), dv[db]);
+      else dk[db] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[c]), dk[db]);
+      if (j < 4) begin(cur, item + 1, qb, j);            // of block b + 2
+      fence();
+    }
   };
   if (i0 < i1) {
-    load(i0, 0);
-    arrived();
-  }
-  const uint32_t tiles = (uint32_t)(uintptr_t)(lvoid)&sT;
-  for (int item = i0; item < i1; ++item) {
-    const int b = (item - i0) & 1;
-    if (item + 1 < i1) load(item + 1, b ^ 1);
-    const int r0 = first + item % nt * kTile;
-    if (__any(r0 < hi && r0 + kTile > lo)) {
-      const bool whole = __all(r0 >= lo && r0 + kTile <= hi);
-#pragma unroll 1
-      for (int qb = 0; qb < 2; ++qb) {
-        const uint32_t tq = tiles + (uint32_t)(b * 2 * Streamed<D>::BYTES + qb * 32 * D * 2), to = tq + Streamed<D>::BYTES;
-        f32x16 s = {}, t = {};
+    for (int i = i0; i < min(i0 + kRing - 1, i1); ++i) load(i);
+    wait_vmcnt<0>();
+    __syncthreads();
+    Scores x, y;
 #pragma unroll
-        for (int kk = 0; kk < NKK; ++kk) {
-          s = mfma32(reader.score(tq, kk), kf[kk], s);
-          t = mfma32(reader.score(to, kk), vf[kk], t);
-        }
-        u32x4 pf[2], df[2];
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int at = 32 * qb + 16 * c + 8 * g;         // the 8 rows of this lane
-          float p[8], d[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -sR[b][0][at + e]));
-          if (!whole)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int i = r0 + at + e;
-              if ((i < lo) | (i >= hi)) p[e] = 0.f;
-            }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[e] = p[e] * (t[8 * c + e] - sR[b][1][at + e]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            pf[c][e] = pack2(p[2 * e], p[2 * e + 1]);
-            df[c][e] = pack2(d[2 * e], d[2 * e + 1]);
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            dv[db] = mfma32(reader.turned(to + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, pf[c]), dv[db]);
-            dk[db] = mfma32(reader.turned(tq + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, df[c]), dk[db]);
-          }
-      }
+    for (int i = 0; i < 4; ++i) {
+      begin(x, i0, 0, i);
+      begin(y, i0, 1, i);
     }
-    if (item + 1 < i1) arrived();
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+      mfma_first(i % 2 == 0 ? x.s : x.t, read_first(block_at(i0, 0) + lane_row, i), i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
+    fence();
+    settle();
+    fence();
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) op[i] = read_first(block_at(i0, 1) + lane_row, i);
+    for (int item = i0; item < i1; ++item) {
+      if (item > i0) {
+        // tile item + 1 is there (tile item + 2 may be on its way), and every wave is done with tile item - 1
+        if (item + 2 < i1) wait_vmcnt<COPIES>();
+        else wait_vmcnt<0>();
+        __syncthreads();
+      }
+      if (item + kRing - 1 < i1) load(item + kRing - 1);
+      const int r0 = first + item % nt * kTile;
+      const bool whole = __all(r0 >= lo && r0 + kTile <= hi);
+      if (!whole) mask(x, r0);
+      step(x, y, item, 0);
+      if (!whole) mask(y, r0 + 32);
+      step(y, x, item, 1);
+    }
   }
 
   // lane: key n of the wave, dims 32 db + 8 rq + 4 g .. + 3
@@ -342,7 +444,7 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradArgs a) {
 
 // --- dQ: a work group takes 128 queries of a query head, each wave 32 ------------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void grad_queries_kernel(GradArgs a) {
+__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kernel(GradArgs a) {
   constexpr int NKK = D / 16, NDB = D / 32;
   __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // keys, values
   SeqArgs q = a.seq;
@@ -360,74 +462,130 @@ __global__ __launch_bounds__(kThreads, 2) void grad_queries_kernel(GradArgs a) {
   bf16x8 qf[NKK], of[NKK];
   {
     const uint16_t *qp = q.q + (u.q0 + at) * q.q_token + h * q.q_head + 8 * g;
-    const uint16_t *op = a.dout + (u.q0 + at) * a.do_token + h * a.do_head + 8 * g;
+    const uint16_t *gp = a.dout + (u.q0 + at) * a.do_token + h * a.do_head + 8 * g;
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) {
       qf[kk] = ld_g16(qp + 16 * kk);
-      of[kk] = ld_g16(op + 16 * kk);
+      of[kk] = ld_g16(gp + 16 * kk);
     }
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(qf[kk]), "+a"(of[kk]));
   }
+  // (see grad_stats_kernel: S and T begin from these; with 64-dim heads, whose two waves on a SIMD leave no registers for them,
+  // they are added to the results)
+  constexpr bool FROM = D == 128;
   const float *sp = a.stats + (int64_t)h * q.n_tokens + u.q0 + at;
   const float lse = sp[0], delta = sp[(int64_t)q.n_tokens * heads];
-  f32x16 dq[NDB];
+  const float lse_log2 = lse == INFINITY ? 0.f : lse * q.scale_log2;      // (a row that sees nothing: its S is masked to -infinity)
+  f32x16 from_s, from_t, dq[NDB];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    from_s[e] = lse;
+    from_t[e] = delta;
+  }
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dq[db] = f32x16{};
-  const Copier<D> copier{lane, wave};
-  const Reader<D> reader(lane);
+
+  const Copier<D> copier(lane, wave);
+  using R = Reader<D>;
+  const R reader(lane);
+  const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
   const uint16_t *kp = q.k + u.k0 * q.k_token + head * q.k_head, *vp = q.v + u.k0 * q.v_token + head * q.v_head;
-  auto load = [&](int t, int b) {
-    const int64_t at = (int64_t)tiles.place(t) * kTile;
-    copier.copy(kp + at * q.k_token, q.k_token, u.nk - (int)at, sT.x[b][0]);
-    copier.copy(vp + at * q.v_token, q.v_token, u.nk - (int)at, sT.x[b][1]);
+  const uint32_t base = lds_addr(&sT);
+  const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.n);
+  auto load = [&](int t) {
+    const int64_t first = (int64_t)tiles.place(t) * kTile;
+    const uint32_t to = base + (uint32_t)(t % kRing * Streamed<D>::SLOT);
+    copier.copy(kp + first * q.k_token, q.k_token, u.nk - (int)first, to);
+    copier.copy(vp + first * q.v_token, q.v_token, u.nk - (int)first, to + Streamed<D>::BYTES);
   };
-  auto arrived = [&] {
+  constexpr int COPIES = 2 * Copier<D>::N;
+  // A step as in grad_keys_kernel, with one second product for each operand: dQ.
+  struct Scores {
+    f32x16 s, t;
+  };
+  constexpr int NF = 2 * NKK, NS = 2 * NDB, EACH = 16 / NF;
+  constexpr int AHEAD = operands_ahead(NF + NS), RO = AHEAD + 1;
+  static_assert((NF + NS) % RO == 0, "the ring of operands");
+  bf16x8 op[RO];
+  auto read_second = [&](uint32_t at, uint32_t at4, int j) { return R::second(at, at4, 0, j / NDB, j % NDB); };
+  auto block_at = [&](int t, int kb) { return base + (uint32_t)(t % kRing * Streamed<D>::SLOT + kb * 32 * D * 2); };
+  auto mask = [&](Scores &x, int key) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (!mine.sees(key + 8 * g + 16 * (e / 8) + e % 8)) x.s[e] = -INFINITY;
+  };
+  auto first_product = [&](Scores &x, int i, bf16x8 w) {
+    if (i < 2 && FROM) mfma_first(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[0] : of[0], i % 2 == 0 ? from_s : from_t);
+    else if (i < 2) mfma_first_zero(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[0] : of[0]);
+    else mfma_first(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[i / 2] : of[i / 2]);
+  };
+  auto step = [&](Scores &cur, Scores &nxt, int t, int kb) {
+    const uint32_t next = block_at(t + kb, 1 - kb) + lane_row, after = block_at(t + 1, kb) + lane_row;
+    const uint32_t here = block_at(t, kb) + turn, here4 = block_at(t, kb) + turn4;
+    auto read_ahead = [&](int i) {
+      const int r = i + AHEAD;
+      op[r % RO] = r < NF ? R::first(next, r) : r < NF + NS ? read_second(here, here4, r - NF) : R::first(after, r - NF - NS);
+    };
+    u32x4 df[2];
+    float d0 = 0.f, last = 0.f;
+    auto rest = [&](int e, float p) {
+      const float d = p * (FROM ? cur.t[e] : cur.t[e] + delta);
+      if (e % 2 == 0) d0 = d;
+      else df[e / 8][e % 8 / 2] = pack2(d0, d);
+    };
+    fence();
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      read_ahead(i);
+      first_product(nxt, i, op[i % RO]);
+      fence();
+#pragma unroll
+      for (int e = EACH * i; e < EACH * (i + 1); ++e) {
+        const float p = __builtin_amdgcn_exp2f(FROM ? cur.s[e] * q.scale_log2 : fmaf(cur.s[e], q.scale_log2, lse_log2));
+        if (e > 0) rest(e - 1, last);
+        last = p;
+      }
+      fence();
+    }
+    rest(15, last);
+#pragma unroll
+    for (int j = 0; j < NS; ++j) {
+      read_ahead(NF + j);
+      dq[j % NDB] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[j / NDB]), dq[j % NDB]);
+      fence();
+    }
+  };
+  if (n_tiles > 0) {
+    for (int t = 0; t < min(kRing - 1, n_tiles); ++t) load(t);
     wait_vmcnt<0>();
     __syncthreads();
-  };
-  if (tiles.n > 0) {
-    load(0, 0);
-    arrived();
-  }
-  const uint32_t base = (uint32_t)(uintptr_t)(lvoid)&sT;
-  for (int t = 0; t < tiles.n; ++t) {
-    const int b = t & 1, place = tiles.place(t);
-    if (t + 1 < tiles.n) load(t + 1, b ^ 1);
-    const bool whole = tiles.whole(place, q.sinks);
-#pragma unroll 1
-    for (int kb = 0; kb < 2; ++kb) {
-      const uint32_t tk = base + (uint32_t)(b * 2 * Streamed<D>::BYTES + kb * 32 * D * 2), tv = tk + Streamed<D>::BYTES;
-      f32x16 s = {}, d = {};
+    Scores x, y;
 #pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) {
-        s = mfma32(reader.score(tk, kk), qf[kk], s);
-        d = mfma32(reader.score(tv, kk), of[kk], d);
+    for (int i = 0; i < NF; ++i) first_product(x, i, R::first(block_at(0, 0) + lane_row, i));
+    fence();
+    settle();
+    fence();
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) op[i] = R::first(block_at(0, 1) + lane_row, i);
+    for (int t = 0; t < n_tiles; ++t) {
+      if (t > 0) {
+        // tile t + 1 is there (tile t + 2 may be on its way), and every wave is done with tile t - 1
+        if (t + 2 < n_tiles) wait_vmcnt<COPIES>();
+        else wait_vmcnt<0>();
+        __syncthreads();
       }
-      u32x4 df[2];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[8 * c + e], q.scale_log2, -lse));
-          x[e] = p * (d[8 * c + e] - delta);
-        }
-        if (!whole)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (!mine.sees(place * kTile + 32 * kb + 16 * c + 8 * g + e)) x[e] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) df[c][e] = pack2(x[2 * e], x[2 * e + 1]);
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-          dq[db] = mfma32(reader.turned(tk + (uint32_t)(c * 16 * D * 2), db), __builtin_bit_cast(bf16x8, df[c]), dq[db]);
+      if (t + kRing - 1 < n_tiles) load(t + kRing - 1);
+      const int place = tiles.place(t);
+      const bool whole = tiles.whole(place, q.sinks);
+      if (!whole) mask(x, place * kTile);
+      step(x, y, t, 0);
+      if (!whole) mask(y, place * kTile + 32);
+      step(y, x, t, 1);
     }
-    if (t + 1 < tiles.n) arrived();
   }
   if (row >= u.nq) return;
-  uint16_t *op = a.dq + (u.q0 + row) * a.dq_token + h * a.dq_head;
+  uint16_t *to = a.dq + (u.q0 + row) * a.dq_token + h * a.dq_head;
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -435,7 +593,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_queries_kernel(GradArgs a) {
       uint2 w;
       w.x = pack2(dq[db][4 * rq] * a.scale, dq[db][4 * rq + 1] * a.scale);
       w.y = pack2(dq[db][4 * rq + 2] * a.scale, dq[db][4 * rq + 3] * a.scale);
-      *reinterpret_cast<uint2 *>(op + 32 * db + 8 * rq + 4 * g) = w;
+      *reinterpret_cast<uint2 *>(to + 32 * db + 8 * rq + 4 * g) = w;
     }
 }
 
