@@ -84,36 +84,36 @@ struct Reader {
   }
 };
 
-// N DMA instructions (see hc_device.h), instruction j from base[j] + a[j] (bytes), behind a wait that covers a base which a
+// N DMA instructions (see hc_device.h) from base + a[j] (bytes) + 1024 j, behind a wait that covers a base which a
 // vector instruction put into its scalar registers just before: 5 wait states, which the compiler does not count for
-// inline assembly.  (base[j] is 1024 j low: the offset counts at both ends.)
+// inline assembly.
 template <int N>
-__device__ __forceinline__ void lds_dma16_each(const uint16_t *const (&base)[N], const uint32_t (&a)[N], uint32_t lds) {
+__device__ __forceinline__ void lds_dma16_settled(const uint16_t *base, const uint32_t (&a)[N], uint32_t lds) {
   static_assert(N == 2 || N == 4, "instructions");
   uint32_t saved;
   if constexpr (N == 2) {
     asm volatile(
         "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %5\n\t"
+        "s_mov_b32 m0, %4\n\t"
         "s_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %4 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "s"(base[0]), "s"(base[1]), "s"(lds)
+        : "v"(a[0]), "v"(a[1]), "s"(base), "s"(lds)
         : "memory");
   } else {
     asm volatile(
         "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %9\n\t"
+        "s_mov_b32 m0, %6\n\t"
         "s_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %6 offset:0x400\n\t"
-        "global_load_lds_dwordx4 %3, %7 offset:0x800\n\t"
-        "global_load_lds_dwordx4 %4, %8 offset:0xc00\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base[0]), "s"(base[1]), "s"(base[2]), "s"(base[3]), "s"(lds)
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base), "s"(lds)
         : "memory");
   }
 }
@@ -133,37 +133,30 @@ __device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uin
       : "memory");
 }
 
-// Copies a tile to LDS by DMA: 64 rows of one head (those behind the last repeat it).  Instruction j of wave w moves 1 KB,
-// the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its 16 bytes.
+// Copies tiles of one tensor to LDS by DMA: 64 rows of one head (those behind the last repeat it).  Instruction j of wave w
+// moves 1 KB, the 8 or 4 rows from (N w + j) 512 / D on; a lane fetches the chunk that belongs at its 16 bytes.  (The base is
+// 4 KB low, so that no offset goes below zero when 1024 j is taken off.)
 template <int D>
 struct Copier {
   static constexpr int RW = 512 / D, N = kTile / RW / kWaves;     // rows of an instruction, instructions of a wave
   int lane, wave;
-  uint32_t chunk[N];         // byte of a row that goes to this lane's place
-  __device__ __forceinline__ Copier(int l, int w) : lane(l), wave(w) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) chunk[j] = (uint32_t)(tswz<D>(N * w * RW + l / (D / 8) + j * RW, l % (D / 8)) * 16);
+  uint32_t token;            // bytes from row to row: below 2^25, so that a row's offset stays below 2^31
+  uint32_t at[N];            // of this lane, in a whole tile
+  __device__ __forceinline__ uint32_t chunk(int j) const {
+    return (uint32_t)(tswz<D>((N * wave + j) * RW + lane / (D / 8), lane % (D / 8)) * 16 + 4096 - 1024 * j);
   }
-  // p: the tile's first row; left: rows from there on.  (A row's offset stays below 2^31: token strides are below 2^24.)
-  __device__ __forceinline__ void copy(const uint16_t *p, int64_t token, int left, uint32_t tile) const {
+  __device__ __forceinline__ Copier(int64_t stride, int l, int w) : lane(l), wave(w), token((uint32_t)stride * 2u) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) at[j] = (uint32_t)((N * w + j) * RW + l / (D / 8)) * token + chunk(j);
+  }
+  // p: the tile's first row; left: rows from there on.
+  __device__ __forceinline__ void copy(const uint16_t *p, int left, uint32_t tile) const {
+    const uint32_t to = tile + (uint32_t)(wave * N * 1024);
+    if (left >= kTile) return lds_dma16_settled<N>(p - 2048, at, to);
     uint32_t a[N];
-    const uint16_t *base[N];
-    const int row = lane / (D / 8);
-    if (left >= kTile) {
-      const uint32_t off = (uint32_t)row * (uint32_t)token * 2u;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        a[j] = chunk[j] + off;
-        base[j] = p + (int64_t)((N * wave + j) * RW) * token - 512 * j;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        a[j] = chunk[j] + (uint32_t)min((N * wave + j) * RW + row, left - 1) * (uint32_t)token * 2u;
-        base[j] = p - 512 * j;
-      }
-    }
-    lds_dma16_each<N>(base, a, tile + (uint32_t)(wave * N * 1024));
+    for (int j = 0; j < N; ++j) a[j] = (uint32_t)min((N * wave + j) * RW + lane / (D / 8), left - 1) * token + chunk(j);
+    lds_dma16_settled<N>(p - 2048, a, to);
   }
 };
 
@@ -231,10 +224,11 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     const uint32_t e = ((uint32_t)j + (uint32_t)q.window) / (uint32_t)q.block * (uint32_t)q.block;
     return (int)min(max((int64_t)e - off, (int64_t)0), (int64_t)u.nq);
   };
-  const int first = from(k0), end = max(first, k0 < q.sinks ? u.nq : until(k_last));
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int first = uniform(from(k0)), end = uniform(max(first, k0 < q.sinks ? u.nq : until(k_last)));
   const int nt = (end - first + kTile - 1) / kTile;    // tiles of every query head
   const int64_t items = (int64_t)nt * q.group;
-  const int i0 = (int)(items * split / a.n_split), i1 = (int)(items * (split + 1) / a.n_split);
+  const int i0 = uniform((int)(items * split / a.n_split)), i1 = uniform((int)(items * (split + 1) / a.n_split));
   const int lo = from(min(key, u.nk - 1)), hi = until(min(key, u.nk - 1));
 
   bf16x8 kf[NKK], vf[NKK];
@@ -253,20 +247,43 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = f32x16{};
 
-  const Copier<D> copier(lane, wave);
+  const Copier<D> copy_q(q.q_token, lane, wave), copy_o(a.do_token, lane, wave);
   using R = Reader<D>;
   const R reader(lane);
-  const int64_t plane = (int64_t)q.n_tokens * q.kv_heads * q.group;
   const uint32_t tiles = lds_addr(&sT), rows = lds_addr(&sR);
   auto slot = [&](int item) { return (uint32_t)((item - i0) % kRing); };
-  // (every wave copies one run of the rows' numbers, so that all have as many copies in flight; two waves copy the same)
+  // The tile that is copied next, moved on from tile to tile and head to head.  (Every wave copies one run of the rows' numbers, so
+  // that all have as many copies in flight; two waves copy the same.)
+  struct {
+    const uint16_t *q, *o;
+    const float *stats;
+    int row;
+  } next_tile;
+  {
+    const int h = head * q.group + i0 / max(nt, 1);
+    next_tile.row = first + i0 % max(nt, 1) * kTile;
+    const int64_t at = u.q0 + next_tile.row;
+    next_tile.q = q.q + at * q.q_token + h * q.q_head;
+    next_tile.o = a.dout + at * a.do_token + h * a.do_head;
+    next_tile.stats = a.stats + (int64_t)(wave % 2 * q.kv_heads * q.group + h) * q.n_tokens + at;
+  }
   auto load = [&](int item) {
-    const int h = head * q.group + item / nt, r0 = first + item % nt * kTile;
     const uint32_t to = tiles + slot(item) * Streamed<D>::SLOT;
-    copier.copy(q.q + (u.q0 + r0) * q.q_token + h * q.q_head, q.q_token, u.nq - r0, to);
-    copier.copy(a.dout + (u.q0 + r0) * a.do_token + h * a.do_head, a.do_token, u.nq - r0, to + Streamed<D>::BYTES);
-    lds_dma4(a.stats + wave % 2 * plane + (int64_t)h * q.n_tokens + u.q0 + r0, u.nq - r0, lane,
-             rows + slot(item) * 512 + wave % 2 * 256);
+    const int left = u.nq - next_tile.row;
+    copy_q.copy(next_tile.q, left, to);
+    copy_o.copy(next_tile.o, left, to + Streamed<D>::BYTES);
+    lds_dma4(next_tile.stats, left, lane, rows + slot(item) * 512 + wave % 2 * 256);
+    next_tile.row += kTile;
+    next_tile.q += kTile * q.q_token;
+    next_tile.o += kTile * a.do_token;
+    next_tile.stats += kTile;
+    if (next_tile.row >= end) {
+      const int back = nt * kTile;
+      next_tile.row = first;
+      next_tile.q += q.q_head - back * q.q_token;
+      next_tile.o += a.do_head - back * a.do_token;
+      next_tile.stats += q.n_tokens - back;
+    }
   };
   constexpr int COPIES = 2 * Copier<D>::N + 1;           // of a wave and tile
 
@@ -367,6 +384,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     fence();
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = read_first(block_at(i0, 1) + lane_row, i);
+    int row = first + i0 % nt * kTile;                   // of the item
     for (int item = i0; item < i1; ++item) {
       if (item > i0) {
         // tile item + 1 is there (tile item + 2 may be on its way), and every wave is done with tile item - 1
@@ -375,12 +393,12 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
         __syncthreads();
       }
       if (item + kRing - 1 < i1) load(item + kRing - 1);
-      const int r0 = first + item % nt * kTile;
-      const bool whole = __all(r0 >= lo && r0 + kTile <= hi);
-      if (!whole) mask(x, r0);
+      const bool whole = __all(row >= lo && row + kTile <= hi);
+      if (!whole) mask(x, row);
       step(x, y, item, 0);
-      if (!whole) mask(y, r0 + 32);
+      if (!whole) mask(y, row + 32);
       step(y, x, item, 1);
+      row = row + kTile < end ? row + kTile : first;
     }
   }
 
@@ -458,7 +476,11 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
   if (!seq_unit<kSeqRows>(q, tile, u)) return;
   const int row = u.row0 + 32 * wave + n, at = min(row, u.nq - 1);
   const Seen mine = seen_by(q, u, at);
-  const KeyTiles tiles(seen_by(q, u, u.row0), seen_by(q, u, min(u.row0 + kSeqRows, u.nq) - 1));
+  KeyTiles tiles(seen_by(q, u, u.row0), seen_by(q, u, min(u.row0 + kSeqRows, u.nq) - 1));
+  tiles.first = __builtin_amdgcn_readfirstlane(tiles.first);
+  tiles.gap = __builtin_amdgcn_readfirstlane(tiles.gap);
+  tiles.lo_end = __builtin_amdgcn_readfirstlane(tiles.lo_end);
+  tiles.hi_start = __builtin_amdgcn_readfirstlane(tiles.hi_start);
   bf16x8 qf[NKK], of[NKK];
   {
     const uint16_t *qp = q.q + (u.q0 + at) * q.q_token + h * q.q_head + 8 * g;
@@ -486,7 +508,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dq[db] = f32x16{};
 
-  const Copier<D> copier(lane, wave);
+  const Copier<D> copy_k(q.k_token, lane, wave), copy_v(q.v_token, lane, wave);
   using R = Reader<D>;
   const R reader(lane);
   const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
@@ -494,10 +516,10 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
   const uint32_t base = lds_addr(&sT);
   const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.n);
   auto load = [&](int t) {
-    const int64_t first = (int64_t)tiles.place(t) * kTile;
+    const int first = tiles.place(t) * kTile;
     const uint32_t to = base + (uint32_t)(t % kRing * Streamed<D>::SLOT);
-    copier.copy(kp + first * q.k_token, q.k_token, u.nk - (int)first, to);
-    copier.copy(vp + first * q.v_token, q.v_token, u.nk - (int)first, to + Streamed<D>::BYTES);
+    copy_k.copy(kp + first * q.k_token, u.nk - first, to);
+    copy_v.copy(vp + first * q.v_token, u.nk - first, to + Streamed<D>::BYTES);
   };
   constexpr int COPIES = 2 * Copier<D>::N;
   // A step as in grad_keys_kernel, with one second product for each operand: dQ.
