@@ -14,7 +14,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libheadcast.so")
 SOURCES = ["hc_runtime.cpp", "hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip",
            "hc_ops.cpp", "hc_rotate.hip", "hc_qcache.hip", "hc_seq.hip", "hc_seq128.hip", "hc_decode.hip",
-           "hc_window.cpp", "hc_norm.hip", "hc_paged.hip", "hc_window_grad.hip"]
+           "hc_window.cpp", "hc_norm.hip", "hc_paged.hip", "hc_window_grad64.hip", "hc_window_grad128.hip"]
 # kernels of the routed attention: finite inputs, and decisions on bit patterns where they overflow
 ROUTED = ("hc_dense.hip", "hc_dense128.hip", "hc_spatial.hip", "hc_merge.hip", "hc_cache.hip", "hc_static.hip")
 
@@ -38,7 +38,7 @@ def build_library(verbose: bool = False) -> str:
     # entry points refuse it in arguments, so their comparisons have to hold for it.
     routed = ["-fno-honor-nans"]
     # MFMA results in vector registers (the online-softmax rescale works on them), except
-    # where the accumulators of 64 queries per wave need the other half of the register file
+    # where the accumulators of 64 queries per wave, or of both gradients of 128 dims, need the other half of the register file
     vgpr_form = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
     tmp = LIB + ".tmp"
 
@@ -54,7 +54,7 @@ def build_library(verbose: bool = False) -> str:
 
     with tempfile.TemporaryDirectory(prefix="headcast_build_") as tdir:
         objs = [os.path.join(tdir, src + ".o") for src in SOURCES]
-        cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip", "hc_window_grad.hip") else vgpr_form)
+        cmds = [[hipcc()] + flags + ([] if src in ("hc_dense128.hip", "hc_seq128.hip", "hc_window_grad128.hip") else vgpr_form)
                 + (routed if src in ROUTED else [])
                 + ["-c", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
         with concurrent.futures.ThreadPoolExecutor(max_workers=len(cmds)) as ex:

@@ -476,7 +476,9 @@ hc_status hc_window_attention_backward(hc_ctx *c, const hc_window_grad_args *g, 
   a.part = (float *)((char *)g->workspace + grad_stat_bytes(p));
   OnDevice on(c->device);
   HC_HIP(c, on.status);
-  return timed_launch(c, (hipStream_t)stream, HC_K_GRADIENT, [&] { return launch_grad(a, p.head_dim, (hipStream_t)stream); });
+  return timed_launch(c, (hipStream_t)stream, HC_K_GRADIENT, [&] {
+    return p.head_dim == 128 ? launch_grad128(a, (hipStream_t)stream) : launch_grad64(a, (hipStream_t)stream);
+  });
 } HC_NO_HOST_MEMORY(c)
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Internal structures of the operators of a model with a sliding window (hc_window.cpp, hc_norm.hip,
-// hc_paged.hip, hc_window_grad.hip, and the kernels of hc_seq.hip and hc_seq128.hip).  Not part of the public ABI.
+// hc_paged.hip, hc_window_grad.h, and the kernels of hc_seq.hip and hc_seq128.hip).  Not part of the public ABI.
 #pragma once
 
 #include "hc_ops.h"
@@ -63,6 +63,7 @@ struct GradArgs {
   int32_t n_split;
   float *part;                   // [key unit][kv head][n_split][2][kGradKeys][d]
 };
-hipError_t launch_grad(const GradArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_grad64(const GradArgs &a, hipStream_t s);
+hipError_t launch_grad128(const GradArgs &a, hipStream_t s);
 
 }  // namespace hc

@@ -1,4 +1,7 @@
-// Gradients of the attention over packed sequences with a window.
+// Gradients of the attention over packed sequences with a window: the kernels, which hc_window_grad64.hip and
+// hc_window_grad128.hip compile for their head sizes, with matrix results in vector and in accumulation registers.
+#pragma once
+
 #include "hc_mask.h"
 #include "hc_window.h"
 
@@ -31,9 +34,10 @@ __device__ __forceinline__ int tswz(int r, int c) {
 
 // Streamed tiles in LDS: a ring of them, two tensors each.  Addresses are a lane's own part, and constants.
 constexpr int kRing = 4;
-// Operands of a step are read some products ahead: each feeds one product of 32 cycles, and a read takes longer than four.  (So
-// many that the ring of them comes around with every step.)
-constexpr int operands_ahead(int products) { return products % 8 == 0 ? 7 : 5; }
+// Operands of a step are read so many products ahead: each feeds one product of 32 cycles, and a read takes longer than
+// four.  (64-dim heads run two waves on a SIMD, which fill in for each other.  The ring of operands comes around with every step.)
+template <int D>
+constexpr int kAhead = D == 128 ? 7 : 3;
 template <int D>
 struct Streamed {
   static constexpr int BYTES = kTile * D * 2, SLOT = 2 * BYTES;
@@ -43,21 +47,30 @@ using lds8 = const __attribute__((address_space(3))) bf16x8 *;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 using ldst = __attribute__((address_space(3))) s16x4 *;
 using ldsf4 = const __attribute__((address_space(3))) f32x4 *;
-// The products S and T, with their stationary operand in the accumulation registers.  (Inline assembly: as the compiler
-// places it, that operand is copied for every product.  tests/test_window_code.py looks at the distance between these products
-// and what reads them.)
+// The products S and T.  128-dim heads: in inline assembly, with their stationary operand in the accumulation registers; as
+// the compiler places it, that operand is copied for every product.  (tests/test_window_code.py looks at the distances between these
+// products, what they read and what reads them.)  64-dim heads have vector registers for everything.
+template <int D>
 __device__ __forceinline__ void mfma_first(f32x16 &c, bf16x8 a, const bf16x8 &b) {
-  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
+  if constexpr (D == 128) asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "a"(b));
+  else c = mfma32(a, b, c);
 }
+template <int D>
 __device__ __forceinline__ void mfma_first(f32x16 &c, bf16x8 a, const bf16x8 &b, const f32x16 &from) {
   // (a product reads what a vector instruction wrote 2 wait states before at the earliest: `from` may be a copy)
-  asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(c) : "v"(a), "a"(b), "v"(from));
+  if constexpr (D == 128) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(c) : "v"(a), "a"(b), "v"(from));
+  else c = mfma32(a, b, from);
 }
-__device__ __forceinline__ void mfma_first_zero(f32x16 &c, bf16x8 a, const bf16x8 &b) {
-  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "a"(b));
+// Matrix results in their registers before vector instructions use them: a 32x32x16 product needs at most 18 wait states.  (The
+// first wait is for copies that the compiler puts before an instruction that names the registers.)
+template <int D>
+__device__ __forceinline__ void settle(f32x16 &s, f32x16 &t) {
+  if constexpr (D != 128) return;
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3");
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s), "+v"(t));
 }
-// Matrix results in their registers before vector instructions use them: a 32x32x16 product needs at most 18 wait states.
-__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3"); }
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int D>
@@ -84,38 +97,21 @@ struct Reader {
   }
 };
 
-// N DMA instructions (see hc_device.h) from base + a[j] (bytes) + 1024 j, behind a wait that covers a base which a
+// Two DMA instructions (see hc_device.h) from base + a (bytes) and base + 1024 + b, behind a wait that covers a base which a
 // vector instruction put into its scalar registers just before: 5 wait states, which the compiler does not count for
 // inline assembly.
-template <int N>
-__device__ __forceinline__ void lds_dma16_settled(const uint16_t *base, const uint32_t (&a)[N], uint32_t lds) {
-  static_assert(N == 2 || N == 4, "instructions");
+__device__ __forceinline__ void lds_dma16_two(const uint16_t *base, uint32_t a, uint32_t b, uint32_t lds) {
   uint32_t saved;
-  if constexpr (N == 2) {
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %4\n\t"
-        "s_nop 4\n\t"
-        "global_load_lds_dwordx4 %1, %3\n\t"
-        "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "s"(base), "s"(lds)
-        : "memory");
-  } else {
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %6\n\t"
-        "s_nop 4\n\t"
-        "global_load_lds_dwordx4 %1, %5\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:0x800\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:0xc00\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "s"(base), "s"(lds)
-        : "memory");
-  }
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %4\n\t"
+      "s_nop 4\n\t"
+      "global_load_lds_dwordx4 %1, %3\n\t"
+      "global_load_lds_dwordx4 %2, %3 offset:0x400\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(a), "v"(b), "s"(base), "s"(lds)
+      : "memory");
 }
 
 // 64 words to LDS by DMA, word i of the `left` behind p (the last repeats) to place i.
@@ -139,24 +135,32 @@ __device__ __forceinline__ void lds_dma4(const float *p, int left, int lane, uin
 template <int D>
 struct Copier {
   static constexpr int RW = 512 / D, N = kTile / RW / kWaves;     // rows of an instruction, instructions of a wave
+  static constexpr int PAIRS = N / 2;
   int lane, wave;
   uint32_t token;            // bytes from row to row: below 2^25, so that a row's offset stays below 2^31
-  uint32_t at[N];            // of this lane, in a whole tile
-  __device__ __forceinline__ uint32_t chunk(int j) const {
-    return (uint32_t)(tswz<D>((N * wave + j) * RW + lane / (D / 8), lane % (D / 8)) * 16 + 4096 - 1024 * j);
+  uint32_t at[N];            // of this lane, in a tile of `rows` rows
+  int rows;
+  __device__ __forceinline__ Copier(int64_t stride, int l, int w) : lane(l), wave(w), token((uint32_t)stride * 2u), rows(0) {
+    of(kTile);
   }
-  __device__ __forceinline__ Copier(int64_t stride, int l, int w) : lane(l), wave(w), token((uint32_t)stride * 2u) {
+  // For a tile with this many rows left.
+  __device__ __forceinline__ void of(int left) {
+    left = min(left, kTile);
+    if (left == rows) return;
+    rows = left;
 #pragma unroll
-    for (int j = 0; j < N; ++j) at[j] = (uint32_t)((N * w + j) * RW + l / (D / 8)) * token + chunk(j);
+    for (int j = 0; j < N; ++j) {
+      const int row = (N * wave + j) * RW + lane / (D / 8);
+      at[j] = (uint32_t)min(row, left - 1) * token + (uint32_t)(tswz<D>(row, lane % (D / 8)) * 16 + 4096 - 1024 * j);
+    }
   }
-  // p: the tile's first row; left: rows from there on.
-  __device__ __forceinline__ void copy(const uint16_t *p, int left, uint32_t tile) const {
-    const uint32_t to = tile + (uint32_t)(wave * N * 1024);
-    if (left >= kTile) return lds_dma16_settled<N>(p - 2048, at, to);
-    uint32_t a[N];
+  // Instructions 2 i and 2 i + 1; p: the tile's first row.
+  __device__ __forceinline__ void copy(const uint16_t *p, uint32_t tile, int i) const {
+    lds_dma16_two(p - 2048 + i * 1024, at[2 * i], at[2 * i + 1], tile + (uint32_t)((wave * N + 2 * i) * 1024));
+  }
+  __device__ __forceinline__ void copy(const uint16_t *p, uint32_t tile) const {
 #pragma unroll
-    for (int j = 0; j < N; ++j) a[j] = (uint32_t)min((N * wave + j) * RW + lane / (D / 8), left - 1) * token + chunk(j);
-    lds_dma16_settled<N>(p - 2048, a, to);
+    for (int i = 0; i < PAIRS; ++i) copy(p, tile, i);
   }
 };
 
@@ -240,14 +244,15 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       kf[kk] = ld_g16(kp + 16 * kk);
       vf[kk] = ld_g16(vp + 16 * kk);
     }
+    if constexpr (D == 128)
 #pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(kf[kk]), "+a"(vf[kk]));
+      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(kf[kk]), "+a"(vf[kk]));
   }
   f32x16 dk[NDB], dv[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = f32x16{};
 
-  const Copier<D> copy_q(q.q_token, lane, wave), copy_o(a.do_token, lane, wave);
+  Copier<D> copy_q(q.q_token, lane, wave), copy_o(a.do_token, lane, wave);
   using R = Reader<D>;
   const R reader(lane);
   const uint32_t tiles = lds_addr(&sT), rows = lds_addr(&sR);
@@ -267,12 +272,21 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     next_tile.o = a.dout + at * a.do_token + h * a.do_head;
     next_tile.stats = a.stats + (int64_t)(wave % 2 * q.kv_heads * q.group + h) * q.n_tokens + at;
   }
-  auto load = [&](int item) {
+  // Copies of one tile, in 2 PAIRS + 1 parts.  There is one for every item, so that as many are always in flight: past the last
+  // the last one is copied again, to a slot that nothing reads.
+  auto prepare = [&] {
+    copy_q.of(u.nq - next_tile.row);
+    copy_o.of(u.nq - next_tile.row);
+  };
+  constexpr int PAIRS = Copier<D>::PAIRS;
+  auto copy = [&](int item, int part) {
     const uint32_t to = tiles + slot(item) * Streamed<D>::SLOT;
-    const int left = u.nq - next_tile.row;
-    copy_q.copy(next_tile.q, left, to);
-    copy_o.copy(next_tile.o, left, to + Streamed<D>::BYTES);
-    lds_dma4(next_tile.stats, left, lane, rows + slot(item) * 512 + wave % 2 * 256);
+    if (part < PAIRS) copy_q.copy(next_tile.q, to, part);
+    else if (part < 2 * PAIRS) copy_o.copy(next_tile.o, to + Streamed<D>::BYTES, part - PAIRS);
+    else lds_dma4(next_tile.stats, u.nq - next_tile.row, lane, rows + slot(item) * 512 + wave % 2 * 256);
+  };
+  auto move_on = [&](int item) {
+    if (item + 1 >= i1) return;
     next_tile.row += kTile;
     next_tile.q += kTile * q.q_token;
     next_tile.o += kTile * a.do_token;
@@ -293,7 +307,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     f32x16 s, t;
   };
   constexpr int NF = 2 * NKK, NS = 4 * NDB, EACH = 16 / NF;      // products of each half; exponentials beside one
-  constexpr int AHEAD = operands_ahead(NF + NS), RO = AHEAD + 1;
+  constexpr int AHEAD = kAhead<D>, RO = AHEAD + 1;
   static_assert((NF + NS) % RO == 0, "the ring of operands");
   bf16x8 op[RO];
   const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
@@ -345,7 +359,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
       read_ahead(i);
-      mfma_first(i % 2 == 0 ? nxt.s : nxt.t, op[i % RO], i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
+      mfma_first<D>(i % 2 == 0 ? nxt.s : nxt.t, op[i % RO], i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
       fence();
 #pragma unroll
       for (int e = EACH * i; e < EACH * (i + 1); ++e) {
@@ -360,6 +374,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     for (int j = 0; j < NS; ++j) {
       read_ahead(NF + j);
       const int c = j / (2 * NDB), db = j / 2 % NDB;
+      // (copies one by one: issued together they would wait for each other, and the products behind them)
+      if (qb == 0 ? j < PAIRS : j <= PAIRS) copy(item + kRing - 1, qb * PAIRS + j);
       if (j % 2 == 0) dv[db] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, pf[c]), dv[db]);
       else dk[db] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[c]), dk[db]);
       if (j < 4) begin(cur, item + 1, qb, j);            // of block b + 2
@@ -367,8 +383,13 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     }
   };
   if (i0 < i1) {
-    for (int i = i0; i < min(i0 + kRing - 1, i1); ++i) load(i);
-    wait_vmcnt<0>();
+    for (int i = i0; i < i0 + kRing - 1; ++i) {
+      prepare();
+#pragma unroll
+      for (int part = 0; part <= 2 * PAIRS; ++part) copy(i, part);
+      move_on(i);
+    }
+    wait_vmcnt<2 * COPIES>();
     __syncthreads();
     Scores x, y;
 #pragma unroll
@@ -378,28 +399,25 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
     }
 #pragma unroll
     for (int i = 0; i < NF; ++i)
-      mfma_first(i % 2 == 0 ? x.s : x.t, read_first(block_at(i0, 0) + lane_row, i), i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
-    fence();
-    settle();
-    fence();
+      mfma_first<D>(i % 2 == 0 ? x.s : x.t, read_first(block_at(i0, 0) + lane_row, i), i % 2 == 0 ? kf[i / 2] : vf[i / 2]);
+    settle<D>(x.s, x.t);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = read_first(block_at(i0, 1) + lane_row, i);
     int row = first + i0 % nt * kTile;                   // of the item
     for (int item = i0; item < i1; ++item) {
-      if (item > i0) {
-        // tile item + 1 is there (tile item + 2 may be on its way), and every wave is done with tile item - 1
-        if (item + 2 < i1) wait_vmcnt<COPIES>();
-        else wait_vmcnt<0>();
-        __syncthreads();
-      }
-      if (item + kRing - 1 < i1) load(item + kRing - 1);
+      // tile item + 1 is there (tile item + 2 may be on its way), and every wave is done with tile item - 1
+      wait_vmcnt<COPIES>();
+      __syncthreads();
+      prepare();
       const bool whole = __all(row >= lo && row + kTile <= hi);
       if (!whole) mask(x, row);
       step(x, y, item, 0);
       if (!whole) mask(y, row + 32);
       step(y, x, item, 1);
+      move_on(item + kRing - 1);
       row = row + kTile < end ? row + kTile : first;
     }
+    wait_vmcnt<0>();              // nothing is on its way to LDS that another work group may have next
   }
 
   // lane: key n of the wave, dims 32 db + 8 rq + 4 g .. + 3
@@ -490,15 +508,13 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       qf[kk] = ld_g16(qp + 16 * kk);
       of[kk] = ld_g16(gp + 16 * kk);
     }
+    if constexpr (D == 128)
 #pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(qf[kk]), "+a"(of[kk]));
+      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(qf[kk]), "+a"(of[kk]));
   }
-  // (see grad_stats_kernel: S and T begin from these; with 64-dim heads, whose two waves on a SIMD leave no registers for them,
-  // they are added to the results)
-  constexpr bool FROM = D == 128;
+  // (see grad_stats_kernel: S and T begin from these)
   const float *sp = a.stats + (int64_t)h * q.n_tokens + u.q0 + at;
   const float lse = sp[0], delta = sp[(int64_t)q.n_tokens * heads];
-  const float lse_log2 = lse == INFINITY ? 0.f : lse * q.scale_log2;      // (a row that sees nothing: its S is masked to -infinity)
   f32x16 from_s, from_t, dq[NDB];
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
@@ -508,18 +524,27 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dq[db] = f32x16{};
 
-  const Copier<D> copy_k(q.k_token, lane, wave), copy_v(q.v_token, lane, wave);
+  Copier<D> copy_k(q.k_token, lane, wave), copy_v(q.v_token, lane, wave);
   using R = Reader<D>;
   const R reader(lane);
   const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
   const uint16_t *kp = q.k + u.k0 * q.k_token + head * q.k_head, *vp = q.v + u.k0 * q.v_token + head * q.v_head;
   const uint32_t base = lds_addr(&sT);
   const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.n);
-  auto load = [&](int t) {
-    const int first = tiles.place(t) * kTile;
+  // (see grad_keys_kernel; past the last tile the last one again)
+  constexpr int PAIRS = Copier<D>::PAIRS;
+  const uint16_t *next_k, *next_v;
+  auto prepare = [&](int t) {
+    const int first = tiles.place(min(t, n_tiles - 1)) * kTile;
+    next_k = kp + first * q.k_token;
+    next_v = vp + first * q.v_token;
+    copy_k.of(u.nk - first);
+    copy_v.of(u.nk - first);
+  };
+  auto copy = [&](int t, int part) {
     const uint32_t to = base + (uint32_t)(t % kRing * Streamed<D>::SLOT);
-    copy_k.copy(kp + first * q.k_token, u.nk - first, to);
-    copy_v.copy(vp + first * q.v_token, u.nk - first, to + Streamed<D>::BYTES);
+    if (part < PAIRS) copy_k.copy(next_k, to, part);
+    else copy_v.copy(next_v, to + Streamed<D>::BYTES, part - PAIRS);
   };
   constexpr int COPIES = 2 * Copier<D>::N;
   // A step as in grad_keys_kernel, with one second product for each operand: dQ.
@@ -527,7 +552,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
     f32x16 s, t;
   };
   constexpr int NF = 2 * NKK, NS = 2 * NDB, EACH = 16 / NF;
-  constexpr int AHEAD = operands_ahead(NF + NS), RO = AHEAD + 1;
+  constexpr int AHEAD = kAhead<D>, RO = AHEAD + 1;
   static_assert((NF + NS) % RO == 0, "the ring of operands");
   bf16x8 op[RO];
   auto read_second = [&](uint32_t at, uint32_t at4, int j) { return R::second(at, at4, 0, j / NDB, j % NDB); };
@@ -538,9 +563,9 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       if (!mine.sees(key + 8 * g + 16 * (e / 8) + e % 8)) x.s[e] = -INFINITY;
   };
   auto first_product = [&](Scores &x, int i, bf16x8 w) {
-    if (i < 2 && FROM) mfma_first(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[0] : of[0], i % 2 == 0 ? from_s : from_t);
-    else if (i < 2) mfma_first_zero(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[0] : of[0]);
-    else mfma_first(i % 2 == 0 ? x.s : x.t, w, i % 2 == 0 ? qf[i / 2] : of[i / 2]);
+    const bf16x8 &b = i % 2 == 0 ? qf[i / 2] : of[i / 2];
+    if (i < 2) mfma_first<D>(i % 2 == 0 ? x.s : x.t, w, b, i % 2 == 0 ? from_s : from_t);
+    else mfma_first<D>(i % 2 == 0 ? x.s : x.t, w, b);
   };
   auto step = [&](Scores &cur, Scores &nxt, int t, int kb) {
     const uint32_t next = block_at(t + kb, 1 - kb) + lane_row, after = block_at(t + 1, kb) + lane_row;
@@ -552,7 +577,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
     u32x4 df[2];
     float d0 = 0.f, last = 0.f;
     auto rest = [&](int e, float p) {
-      const float d = p * (FROM ? cur.t[e] : cur.t[e] + delta);
+      const float d = p * cur.t[e];
       if (e % 2 == 0) d0 = d;
       else df[e / 8][e % 8 / 2] = pack2(d0, d);
     };
@@ -564,7 +589,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       fence();
 #pragma unroll
       for (int e = EACH * i; e < EACH * (i + 1); ++e) {
-        const float p = __builtin_amdgcn_exp2f(FROM ? cur.s[e] * q.scale_log2 : fmaf(cur.s[e], q.scale_log2, lse_log2));
+        const float p = __builtin_amdgcn_exp2f(cur.s[e] * q.scale_log2);
         if (e > 0) rest(e - 1, last);
         last = p;
       }
@@ -574,30 +599,30 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
       read_ahead(NF + j);
+      if (j < PAIRS) copy(t + kRing - 1, kb * PAIRS + j);
       dq[j % NDB] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[j / NDB]), dq[j % NDB]);
       fence();
     }
   };
   if (n_tiles > 0) {
-    for (int t = 0; t < min(kRing - 1, n_tiles); ++t) load(t);
-    wait_vmcnt<0>();
+    for (int t = 0; t < kRing - 1; ++t) {
+      prepare(t);
+#pragma unroll
+      for (int part = 0; part < 2 * PAIRS; ++part) copy(t, part);
+    }
+    wait_vmcnt<2 * COPIES>();
     __syncthreads();
     Scores x, y;
 #pragma unroll
     for (int i = 0; i < NF; ++i) first_product(x, i, R::first(block_at(0, 0) + lane_row, i));
-    fence();
-    settle();
-    fence();
+    settle<D>(x.s, x.t);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = R::first(block_at(0, 1) + lane_row, i);
     for (int t = 0; t < n_tiles; ++t) {
-      if (t > 0) {
-        // tile t + 1 is there (tile t + 2 may be on its way), and every wave is done with tile t - 1
-        if (t + 2 < n_tiles) wait_vmcnt<COPIES>();
-        else wait_vmcnt<0>();
-        __syncthreads();
-      }
-      if (t + kRing - 1 < n_tiles) load(t + kRing - 1);
+      // tile t + 1 is there (tile t + 2 may be on its way), and every wave is done with tile t - 1
+      wait_vmcnt<COPIES>();
+      __syncthreads();
+      prepare(t + kRing - 1);
       const int place = tiles.place(t);
       const bool whole = tiles.whole(place, q.sinks);
       if (!whole) mask(x, place * kTile);
@@ -605,6 +630,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       if (!whole) mask(y, place * kTile + 32);
       step(y, x, t, 1);
     }
+    wait_vmcnt<0>();
   }
   if (row >= u.nq) return;
   uint16_t *to = a.dq + (u.q0 + row) * a.dq_token + h * a.dq_head;
@@ -635,9 +661,4 @@ hipError_t launch(const GradArgs &a, hipStream_t s) {
 }
 
 }  // namespace
-
-hipError_t launch_grad(const GradArgs &a, int head_dim, hipStream_t s) {
-  return head_dim == 128 ? launch<128>(a, s) : launch<64>(a, s);
-}
-
 }  // namespace hc
