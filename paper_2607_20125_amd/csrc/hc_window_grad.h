@@ -301,12 +301,15 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
   };
   constexpr int COPIES = 2 * Copier<D>::N + 1;           // of a wave and tile
 
-  // A step is block b of 32 rows: beside the products S and T of block b + 1 go the exponentials of block b, then
-  // its products dV and dK.  Operands are read AHEAD products ahead.
+  // A step is block b of 32 rows: beside the products S and T of block b + 1 go the last exponentials of block b and what becomes
+  // of them, beside its products dV and dK the first LATE exponentials of block b + 1, from the product on behind which S is there.
+  // (All beside the first products they take longer than those: 16 of 16 cycles.)  Operands are read AHEAD products ahead.
   struct Scores {
     f32x16 s, t;
   };
-  constexpr int NF = 2 * NKK, NS = 4 * NDB, EACH = 16 / NF;      // products of each half; exponentials beside one
+  constexpr int NF = 2 * NKK, NS = 4 * NDB, EACH = 16 / NF;      // products of each half; elements of a first one
+  constexpr int FROM = 3, PER = D == 128 ? 1 : 2, LATE = (NS - FROM) * PER;
+  static_assert(LATE <= 16, "exponentials");
   constexpr int AHEAD = kAhead<D>, RO = AHEAD + 1;
   static_assert((NF + NS) % RO == 0, "the ring of operands");
   bf16x8 op[RO];
@@ -327,13 +330,14 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       x.t[4 * i + e] = d[e];
     }
   };
-  // rows that do not see this lane's key get no weight
+  // rows that do not see this lane's key get no weight, whether their exponential is there already or not
   auto mask = [&](Scores &x, int row) {
     const uint32_t from = (uint32_t)(row + 8 * g - lo), width = (uint32_t)(hi - lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (from + (uint32_t)(16 * (e / 8) + e % 8) >= width) x.s[e] = -INFINITY;
+      if (from + (uint32_t)(16 * (e / 8) + e % 8) >= width) x.s[e] = e < LATE ? 0.f : -INFINITY;
   };
+  auto weight = [&](Scores &x, int e) { x.s[e] = __builtin_amdgcn_exp2f(x.s[e] * q.scale_log2); };
   auto step = [&](Scores &cur, Scores &nxt, int item, int qb) {
     const int item1 = item + qb;                         // of block b + 1
     const uint32_t next = block_at(item1, 1 - qb) + lane_row, after = block_at(item + 1, qb) + lane_row;
@@ -343,15 +347,14 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       op[r % RO] = r < NF ? read_first(next, r) : r < NF + NS ? read_second(here, here4, r - NF) : read_first(after, r - NF - NS);
     };
     u32x4 pf[2], df[2];
-    float p0 = 0.f, d0 = 0.f, last = 0.f;
+    float d0 = 0.f;
     // what is left of an element once its exponential is there
-    auto rest = [&](int e, float p) {
-      const float d = p * cur.t[e];
+    auto rest = [&](int e) {
+      const float d = cur.s[e] * cur.t[e];
       if (e % 2 == 0) {
-        p0 = p;
         d0 = d;
       } else {
-        pf[e / 8][e % 8 / 2] = pack2(p0, p);
+        pf[e / 8][e % 8 / 2] = pack2(cur.s[e - 1], cur.s[e]);
         df[e / 8][e % 8 / 2] = pack2(d0, d);
       }
     };
@@ -363,13 +366,12 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       fence();
 #pragma unroll
       for (int e = EACH * i; e < EACH * (i + 1); ++e) {
-        const float p = __builtin_amdgcn_exp2f(cur.s[e] * q.scale_log2);
-        if (e > 0) rest(e - 1, last);
-        last = p;
+        if (e >= LATE) weight(cur, e);
+        if (e > 0) rest(e - 1);
       }
       fence();
     }
-    rest(15, last);
+    rest(15);
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
       read_ahead(NF + j);
@@ -380,6 +382,11 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       else dk[db] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[c]), dk[db]);
       if (j < 4) begin(cur, item + 1, qb, j);            // of block b + 2
       fence();
+      if (j >= FROM) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) weight(nxt, (j - FROM) * PER + e);
+        fence();
+      }
     }
   };
   if (i0 < i1) {
@@ -404,6 +411,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = read_first(block_at(i0, 1) + lane_row, i);
     int row = first + i0 % nt * kTile;                   // of the item
+#pragma unroll
+    for (int e = 0; e < LATE; ++e) weight(x, e);
     for (int item = i0; item < i1; ++item) {
       // tile item + 1 is there (tile item + 2 may be on its way), and every wave is done with tile item - 1
       wait_vmcnt<COPIES>();
@@ -414,8 +423,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       step(x, y, item, 0);
       if (!whole) mask(y, row + 32);
       step(y, x, item, 1);
-      move_on(item + kRing - 1);
       row = row + kTile < end ? row + kTile : first;
+      move_on(item + kRing - 1);
     }
     wait_vmcnt<0>();              // nothing is on its way to LDS that another work group may have next
   }
@@ -552,6 +561,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
     f32x16 s, t;
   };
   constexpr int NF = 2 * NKK, NS = 2 * NDB, EACH = 16 / NF;
+  constexpr int FROM = 3, PER = 2, LATE = (NS - FROM) * PER;
   constexpr int AHEAD = kAhead<D>, RO = AHEAD + 1;
   static_assert((NF + NS) % RO == 0, "the ring of operands");
   bf16x8 op[RO];
@@ -560,13 +570,14 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
   auto mask = [&](Scores &x, int key) {
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (!mine.sees(key + 8 * g + 16 * (e / 8) + e % 8)) x.s[e] = -INFINITY;
+      if (!mine.sees(key + 8 * g + 16 * (e / 8) + e % 8)) x.s[e] = e < LATE ? 0.f : -INFINITY;
   };
   auto first_product = [&](Scores &x, int i, bf16x8 w) {
     const bf16x8 &b = i % 2 == 0 ? qf[i / 2] : of[i / 2];
     if (i < 2) mfma_first<D>(i % 2 == 0 ? x.s : x.t, w, b, i % 2 == 0 ? from_s : from_t);
     else mfma_first<D>(i % 2 == 0 ? x.s : x.t, w, b);
   };
+  auto weight = [&](Scores &x, int e) { x.s[e] = __builtin_amdgcn_exp2f(x.s[e] * q.scale_log2); };
   auto step = [&](Scores &cur, Scores &nxt, int t, int kb) {
     const uint32_t next = block_at(t + kb, 1 - kb) + lane_row, after = block_at(t + 1, kb) + lane_row;
     const uint32_t here = block_at(t, kb) + turn, here4 = block_at(t, kb) + turn4;
@@ -575,9 +586,9 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       op[r % RO] = r < NF ? R::first(next, r) : r < NF + NS ? read_second(here, here4, r - NF) : R::first(after, r - NF - NS);
     };
     u32x4 df[2];
-    float d0 = 0.f, last = 0.f;
-    auto rest = [&](int e, float p) {
-      const float d = p * cur.t[e];
+    float d0 = 0.f;
+    auto rest = [&](int e) {
+      const float d = cur.s[e] * cur.t[e];
       if (e % 2 == 0) d0 = d;
       else df[e / 8][e % 8 / 2] = pack2(d0, d);
     };
@@ -589,19 +600,23 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       fence();
 #pragma unroll
       for (int e = EACH * i; e < EACH * (i + 1); ++e) {
-        const float p = __builtin_amdgcn_exp2f(cur.s[e] * q.scale_log2);
-        if (e > 0) rest(e - 1, last);
-        last = p;
+        if (e >= LATE) weight(cur, e);
+        if (e > 0) rest(e - 1);
       }
       fence();
     }
-    rest(15, last);
+    rest(15);
 #pragma unroll
     for (int j = 0; j < NS; ++j) {
       read_ahead(NF + j);
       if (j < PAIRS) copy(t + kRing - 1, kb * PAIRS + j);
       dq[j % NDB] = mfma32(op[(NF + j) % RO], __builtin_bit_cast(bf16x8, df[j / NDB]), dq[j % NDB]);
       fence();
+      if (j >= FROM) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e) weight(nxt, (j - FROM) * PER + e);
+        fence();
+      }
     }
   };
   if (n_tiles > 0) {
@@ -618,6 +633,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
     settle<D>(x.s, x.t);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) op[i] = R::first(block_at(0, 1) + lane_row, i);
+#pragma unroll
+    for (int e = 0; e < LATE; ++e) weight(x, e);
     for (int t = 0; t < n_tiles; ++t) {
       // tile t + 1 is there (tile t + 2 may be on its way), and every wave is done with tile t - 1
       wait_vmcnt<COPIES>();
