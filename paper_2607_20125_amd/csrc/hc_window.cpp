@@ -253,8 +253,14 @@ hc_status grad_plan(hc_ctx *c, const hc_window_grad_args *g, GradArgs &a) {
   const bool alike = (p->cu_k ? p->cu_k : p->cu_q) == nullptr;
   const int64_t k_tiles = unit_room(p->n_keys, p->n_seqs, 1, kGradKeys, alike);
   const int64_t units = k_tiles * p->n_kv_heads;
-  const int64_t rows = (int64_t)p->n_tokens / p->n_seqs * a.seq.group / 64;      // tiles of them that a unit walks, about
-  a.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / std::max<int64_t>(units, 1), rows / 4, 16}));
+  // Key units are cut into pieces of rows until 512 work groups run (two for each CU with 64-dim heads, two rounds with 128), but
+  // no piece is shorter than 4 tiles of rows: a partial gradient costs two writes, two reads and a launch.  512, 768 and 1024: one
+  // sequence of 2048, 4 x 4 heads of 128 dims 118, 136 and 150 us; two heads of 4096, 64 dims 87, 95 and 103; six prompts of up to
+  // 1450, window 512, 4 x 3 heads of 64 dims 77, 74 and 72 (256: 122, 89 and 125).
+  int64_t queries = (int64_t)p->n_tokens / p->n_seqs;            // that see a key, about
+  if (p->window > 0) queries = std::min(queries, (int64_t)p->window + p->causal_block + kGradKeys);
+  const int64_t tiles = queries * a.seq.group / 64;
+  a.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(units, 1), tiles / 4, 16}));
   if (!good_grid(q_tiles * p->n_heads) || !good_grid(units * std::max(a.n_split, 16)) ||
       !good_grid((int64_t)p->n_tokens * p->n_heads / (256 / 16) + 1))
     return fail(c, HC_E_INVAL, "too many rows for one call");

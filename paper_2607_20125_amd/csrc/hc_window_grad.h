@@ -244,9 +244,6 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       kf[kk] = ld_g16(kp + 16 * kk);
       vf[kk] = ld_g16(vp + 16 * kk);
     }
-    if constexpr (D == 128)
-#pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(kf[kk]), "+a"(vf[kk]));
   }
   f32x16 dk[NDB], dv[NDB];
 #pragma unroll
@@ -396,6 +393,10 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
       for (int part = 0; part <= 2 * PAIRS; ++part) copy(i, part);
       move_on(i);
     }
+    // (the stationary operands, loaded before, are there only now)
+    if constexpr (D == 128)
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(kf[kk]), "+a"(vf[kk]));
     wait_vmcnt<2 * COPIES>();
     __syncthreads();
     Scores x, y;
@@ -517,9 +518,6 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
       qf[kk] = ld_g16(qp + 16 * kk);
       of[kk] = ld_g16(gp + 16 * kk);
     }
-    if constexpr (D == 128)
-#pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(qf[kk]), "+a"(of[kk]));
   }
   // (see grad_stats_kernel: S and T begin from these)
   const float *sp = a.stats + (int64_t)h * q.n_tokens + u.q0 + at;
@@ -625,6 +623,9 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
 #pragma unroll
       for (int part = 0; part < 2 * PAIRS; ++part) copy(t, part);
     }
+    if constexpr (D == 128)
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) asm volatile("" : "+a"(qf[kk]), "+a"(of[kk]));
     wait_vmcnt<2 * COPIES>();
     __syncthreads();
     Scores x, y;
