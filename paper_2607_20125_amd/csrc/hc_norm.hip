@@ -149,11 +149,11 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a) {
 // by the launch's work groups, adding dw up in registers; a work group's sums, joined in LDS, go to one row of the
 // workspace, and a second launch adds those rows up in a fixed order.
 // ---------------------------------------------------------------------------
-constexpr int kBackInFlight = 2;
 
 template <typename XT, typename OT, bool HALVES>
 __global__ __launch_bounds__(kThreads) void norm_rotate_backward_kernel(NormArgs a) {
   using I = Item<HALVES>;
+  constexpr int kBackInFlight = HALVES ? 1 : 2;       // heads (with both ends of 8 pairs, two cost half of the waves)
   __shared__ float sw[kThreads * I::NV * 8];
   const RotateArgs &r = a.rotate;
   const int per_group = kThreads >> a.lane_bits, slot = threadIdx.x >> a.lane_bits;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads) void norm_weights_kernel(NormArgs a) {
   const int64_t rows = norm_parts(a, blockIdx.y);
   const float *p = a.part + (blockIdx.y ? norm_parts(a, 0) : 0) * a.rotate.head_dim + dim;
   float sum = 0.f;
-#pragma unroll 4
+#pragma unroll 16
   for (int64_t i = first; i < rows; i += 32) sum += p[i * a.rotate.head_dim];
   sw[threadIdx.x] = sum;
   __syncthreads();

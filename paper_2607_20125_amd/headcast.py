@@ -676,6 +676,9 @@ class Context:
     @staticmethod
     def _apart(outs, others):
         """Refuses two written tensors at one address, and one at another tensor's."""
+        written = {p for _, p in outs if p}
+        if len(written) == len([p for _, p in outs if p]) and written.isdisjoint([p for _, p in others]):
+            return
         for i, (name, p) in enumerate(outs):
             for other, q in outs[i + 1:] + others:
                 if p == q and p:
@@ -728,22 +731,23 @@ class Context:
         if len(dxs) != len(xs) or len(dws) != len(xs):
             raise ValueError("as many dx and dweight as x")
         args, found = self._norm_args(xs, douts, weights, axis_dims, positions, grid, frame0, theta, halves, joint, inverse, eps)
-        tensors, written, read = [], [], []
-        for i, ((shape, xp, op, wp), dxt, dw) in enumerate(zip(found, dxs, dws)):
-            dp = self._rows("dx", dxt, (xs[0].dtype,), shape)
+        tensors, dxp, written, read = [], [], [], []
+        dx_types = (xs[0].dtype,)
+        for (shape, xp, op, wp), dxt, dw in zip(found, dxs, dws):
+            dp = self._rows("dx", dxt, dx_types, shape)
             if dw is not None and (dw.dtype is not torch.float32 or dw.shape != shape[2:] or not dw.is_contiguous()
                                    or dw.get_device() != self.device):
                 raise ValueError(f"dweight: expected a contiguous float32 tensor of shape ({shape[2]},) on cuda:{self.device}")
             dwp = 0 if dw is None else dw.data_ptr()
             tensors.append(_PACK_NORM_GRAD(xp[0], op[0], wp, dp[0], dwp, xp[1], xp[2], op[1], op[2], dp[1], dp[2], shape[1]))
-            written += [(f"dx[{i}]", dp[0]), (f"dweight[{i}]", dwp)]
             # (a tensor's dx may be its own x or dout, but not the other's)
-            read += [("the weights", wp)]
-            for j, (_, xq, oq, _) in enumerate(found):
-                if j != i and dp[0] in (xq[0], oq[0]) and shape[0]:
-                    raise ValueError(f"dx[{i}] overlaps an input of the other tensor")
+            dxp.append(dp[0])
+            written += ("dx", dp[0]), ("dweight", dwp)
+            read.append(("a weight", wp))
         if xs[0].shape[0]:
             self._apart(written, read)
+            if len(found) == 2 and (dxp[0] in (found[1][1][0], found[1][2][0]) or dxp[1] in (found[0][1][0], found[0][2][0])):
+                raise ValueError("a tensor's dx overlaps an input of the other")
         tensors = b"".join(tensors)
         need = self._need
         status = lib.hc_norm_rotate_workspace(self._h, args, tensors, len(found), need)
