@@ -514,8 +514,9 @@ hc_status hc_paged_append(hc_ctx *ctx, const hc_pages *pages, const hc_page_tabl
                           const hc_qcache_rows *rows, hc_stream stream);
 
 /* Attention of new queries (a chunk of each sequence, or single tokens) over its first kv_len[s] slots, m =
- * kv_len[s] in the mask above.  Roundings and the range of logits are those of hc_packed_attention.  Slots behind kv_len
- * and absent pages are not read. */
+ * kv_len[s] in the mask above.  Roundings and the range of logits are those of hc_packed_attention.  What slots behind
+ * kv_len, absent pages and pages of no table hold does not count, whatever it is; a NaN or infinity in a sequence's own
+ * slots may reach any of its queries, hidden or not, and no other sequence's. */
 typedef struct {
   const void *q;             /* bf16 [n_tokens][n_heads][head_dim]                        */
   void *out;                 /* bf16, the same shape; may be q itself with the same strides,

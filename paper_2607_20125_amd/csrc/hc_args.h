@@ -162,7 +162,7 @@ inline hc_status check_rotation(hc_ctx *c, const hc_rotate_args *p, RotateArgs &
     return fail(c, HC_E_INVAL, "axis_dims must add up to a multiple of 16 up to head_dim");
   if (p->positions) {
     if (!aligned4(p->positions)) return fail(c, HC_E_INVAL, "positions must be 4-byte aligned");
-  } else {
+  } else if (p->n_tokens > 0) {                    // (no positions of no tokens may well be a NULL)
     if (p->n_axes != 3 || p->grid_h < 1 || p->grid_w < 1)
       return fail(c, HC_E_INVAL, "positions from the grid need three axes, grid_h and grid_w");
     const int64_t frames = p->n_tokens / ((int64_t)p->grid_h * p->grid_w) + 1;

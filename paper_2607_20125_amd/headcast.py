@@ -764,7 +764,7 @@ class Context:
 
     def pages(self, n_pages: int, page_tokens: int, n_heads: int, head_dim: int) -> Pages:
         """New pages on this context's device, a head's tokens of a page side by side.  (Their memory is not cleared:
-        what no table and length names is not read.)"""
+        what no table and length names does not count.)"""
         if torch is None:
             _use_torch()
         shape = (n_pages, n_heads, page_tokens, head_dim)

@@ -191,6 +191,17 @@ void norm_refusals() {
       }
 }
 
+void no_tokens() {
+  Ctx x;
+  Norm r = good_norm();
+  r.a.rotate.n_axes = 1;
+  r.a.rotate.axis_dims[0] = 128; r.a.rotate.axis_dims[1] = r.a.rotate.axis_dims[2] = 0;
+  CHECK(hc_norm_rotate(x.c, &r.a, r.t, r.n, nullptr) == HC_E_INVAL);         // neither positions nor a grid
+  r.a.rotate.n_tokens = 0;
+  CHECK(hc_norm_rotate(x.c, &r.a, r.t, r.n, nullptr) == HC_OK);
+  CHECK(hc_norm_rotate_backward(x.c, &r.a, r.g, r.n, nullptr, 0, nullptr) == HC_OK && normed.groups == 0);
+}
+
 // --- pages ------------------------------------------------------------------------------------
 struct Paged {
   hc_pages p;
@@ -439,6 +450,7 @@ void call_devices() {
 int main(int argc, char **argv) {
   const std::string name = argc > 1 ? argv[1] : "";
   if (name == "norm_refusals") norm_refusals();
+  else if (name == "no_tokens") no_tokens();
   else if (name == "paged_refusals") paged_refusals();
   else if (name == "window_refusals") window_refusals();
   else if (name == "rooms") rooms();

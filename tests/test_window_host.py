@@ -199,3 +199,10 @@ def test_window_refusals(ctx):
         ctx.window_attention(leaf, k, v)
     with torch.no_grad():
         taken(lambda: ctx.window_attention(leaf, k, v))
+
+
+def test_no_positions_of_no_tokens(window_check):
+    """An empty tensor of positions has no address, which stands for the grid where there are tokens."""
+    run = subprocess.run([window_check, "no_tokens"], capture_output=True, text=True, timeout=60,
+                         env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+    assert run.returncode == 0, run.stdout + run.stderr
