@@ -267,7 +267,7 @@ hc_status grad_plan(hc_ctx *c, const hc_window_grad_args *g, GradArgs &a) {
   if (p->window > 0) queries = std::min(queries, (int64_t)p->window + p->causal_block + kGradKeys);
   const int64_t tiles = queries * a.seq.group / 64;
   a.n_split = (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(units, 1), tiles / 4, 16}));
-  if (!good_grid(q_tiles * p->n_heads) || !good_grid(units * std::max(a.n_split, 16)) ||
+  if (!good_grid(q_tiles * p->n_heads + units * std::max(a.n_split, 16)) ||
       !good_grid((int64_t)p->n_tokens * p->n_heads / (256 / 16) + 1))
     return fail(c, HC_E_INVAL, "too many rows for one call");
   a.seq.tiles = (int)q_tiles;

@@ -43,6 +43,12 @@ struct Streamed {
   static constexpr int BYTES = kTile * D * 2, SLOT = 2 * BYTES;
   uint16_t x[kRing][2][kTile * D];
 };
+// (The numbers beside the rows are those of keys' units: the rows' logarithms, rowsum(dO O).)
+template <int D>
+struct Shared {
+  __attribute__((aligned(1024))) Streamed<D> tiles;
+  __attribute__((aligned(1024))) float rows[kRing][2][kTile];
+};
 using lds8 = const __attribute__((address_space(3))) bf16x8 *;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 using ldst = __attribute__((address_space(3))) s16x4 *;
@@ -202,15 +208,13 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 
 // --- dK and dV: a work group takes 128 keys of a key head, each wave 32 --------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(GradArgs a) {
+__device__ __forceinline__ void keys_unit(const GradArgs &a, int block, Shared<D> &lds) {
   constexpr int NKK = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // queries, output gradients
-  __shared__ __attribute__((aligned(1024))) float sR[kRing][2][kTile];      // their logarithms, rowsum(dO O)
   const SeqArgs &q = a.seq;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
-  const int split = blockIdx.x % a.n_split;
-  const int unit = blockIdx.x / a.n_split;
+  const int split = block % a.n_split;
+  const int unit = block / a.n_split;
   const int tile = __builtin_amdgcn_readfirstlane(unit / q.kv_heads), head = unit - tile * q.kv_heads;
   SeqUnit u;
   if (!seq_unit<kGradKeys, true>(q, tile, u)) return;
@@ -252,7 +256,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_keys_kernel(G
   Copier<D> copy_q(q.q_token, lane, wave), copy_o(a.do_token, lane, wave);
   using R = Reader<D>;
   const R reader(lane);
-  const uint32_t tiles = lds_addr(&sT), rows = lds_addr(&sR);
+  const uint32_t tiles = lds_addr(&lds.tiles), rows = lds_addr(&lds.rows);
   auto slot = [&](int item) { return (uint32_t)((item - i0) % kRing); };
   // The tile that is copied next, moved on from tile to tile and head to head.  (Every wave copies one run of the rows' numbers, so
   // that all have as many copies in flight; two waves copy the same.)
@@ -490,16 +494,15 @@ __global__ __launch_bounds__(256) void grad_merge_kernel(GradArgs a) {
 
 // --- dQ: a work group takes 128 queries of a query head, each wave 32 ------------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kernel(GradArgs a) {
+__device__ __forceinline__ void queries_unit(const GradArgs &a, int block, Shared<D> &lds) {
   constexpr int NKK = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(1024))) Streamed<D> sT;        // keys, values
   SeqArgs q = a.seq;
   const int group = q.group;
   q.group = 1;                       // rows are the queries of one head
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, g = lane >> 5;
   const int heads = q.kv_heads * group;
-  const int tile = __builtin_amdgcn_readfirstlane((int)blockIdx.x / heads), h = (int)blockIdx.x - tile * heads, head = h / group;
+  const int tile = __builtin_amdgcn_readfirstlane(block / heads), h = block - tile * heads, head = h / group;
   SeqUnit u;
   if (!seq_unit<kSeqRows>(q, tile, u)) return;
   const int row = u.row0 + 32 * wave + n, at = min(row, u.nq - 1);
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
   const R reader(lane);
   const uint32_t lane_row = reader.row, turn = reader.turn, turn4 = reader.turn4;
   const uint16_t *kp = q.k + u.k0 * q.k_token + head * q.k_head, *vp = q.v + u.k0 * q.v_token + head * q.v_head;
-  const uint32_t base = lds_addr(&sT);
+  const uint32_t base = lds_addr(&lds.tiles);
   const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.n);
   // (see grad_keys_kernel; past the last tile the last one again)
   constexpr int PAIRS = Copier<D>::PAIRS;
@@ -663,18 +666,25 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_queries_kerne
     }
 }
 
+// Both in one launch, units of keys first, which are the longer ones: neither needs the other, and the last of the ones run beside
+// the first of the others.  Under a causal mask early keys and late queries have most to do, so that queries come from the last on.
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_kernel(GradArgs a) {
+  __shared__ Shared<D> lds;
+  const int keys = a.key_tiles * a.seq.kv_heads * a.n_split, block = (int)blockIdx.x;
+  if (block < keys) keys_unit<D>(a, block, lds);
+  else queries_unit<D>(a, (int)gridDim.x - 1 - block, lds);
+}
+
 template <int D>
 hipError_t launch(const GradArgs &a, hipStream_t s) {
   const int heads = a.seq.kv_heads * a.seq.group;
   const int64_t rows = (int64_t)a.seq.n_tokens * heads * (D / 8);
   if (rows > 0) hipLaunchKernelGGL(grad_stats_kernel<D>, dim3((uint32_t)((rows + 255) / 256)), dim3(256), 0, s, a);
-  if (a.key_tiles > 0) {
-    hipLaunchKernelGGL(grad_keys_kernel<D>, dim3((uint32_t)(a.key_tiles * a.seq.kv_heads * a.n_split)), dim3(kThreads), 0, s, a);
-    if (a.n_split > 1)
-      hipLaunchKernelGGL(grad_merge_kernel<D>, dim3((uint32_t)(a.key_tiles * a.seq.kv_heads * (kGradKeys * D / 1024))), dim3(256), 0, s, a);
-  }
-  if (a.seq.tiles > 0)
-    hipLaunchKernelGGL(grad_queries_kernel<D>, dim3((uint32_t)(a.seq.tiles * heads)), dim3(kThreads), 0, s, a);
+  const int64_t blocks = (int64_t)a.key_tiles * a.seq.kv_heads * a.n_split + (int64_t)a.seq.tiles * heads;
+  hipLaunchKernelGGL(grad_kernel<D>, dim3((uint32_t)blocks), dim3(kThreads), 0, s, a);
+  if (a.n_split > 1 && a.key_tiles > 0)
+    hipLaunchKernelGGL(grad_merge_kernel<D>, dim3((uint32_t)(a.key_tiles * a.seq.kv_heads * (kGradKeys * D / 1024))), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -10,7 +10,7 @@ import pytest
 
 import test_dense128_scores as W
 
-KERNELS = {"window_attn128_kernel": 2, "grad_keys_kernel": 2, "grad_queries_kernel": 2}
+KERNELS = {"window_attn128_kernel": 2, "11grad_kernel": 2}
 
 
 @pytest.fixture(scope="module")
@@ -38,7 +38,7 @@ def test_no_instruction_touches_a_score_too_early(listings):
         if "ILi64E" in name:              # none by hand
             continue
         products, bad = W.too_early(code)
-        assert products >= (64 if "window_attn128_kernel" in name else 24), (name, products)
+        assert products >= (64 if "window_attn128_kernel" in name else 48), (name, products)
         assert not bad, (name, bad[:5])
 
 
