@@ -13,7 +13,8 @@ using namespace dev;
 // 8 dims of a token (or both ends of 8 pairs half a head apart) in several heads, so that an angle is
 // computed once; the 8, 16 or 32 lanes of a head add their squares up in the vector unit (lanes are
 // mirrored and swapped in place: no LDS).  Sums, the norm and the rotation are in 32 bits, rounded once
-// at the end.
+// at the end.  A thread has 4 heads' loads in flight.  Queries and keys of a 720P block (10800 tokens, 12 + 12 heads of 128
+// dims, bf16): 24 us, 5.4 TB/s, the rotation alone 23.
 // ---------------------------------------------------------------------------
 constexpr int kThreads = kNormThreads, kInFlight = kNormInFlight;
 
@@ -147,7 +148,9 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a) {
 //
 // Bound by memory: x and dy in, dx out.  Threads own what they own in the forward pass and walk the tokens
 // by the launch's work groups, adding dw up in registers; a work group's sums, joined in LDS, go to one row of the
-// workspace, and a second launch adds those rows up in a fixed order.
+// workspace, and a second launch adds those rows up in a fixed order, so that results repeat bit for bit.  Two heads in
+// flight, or one with pairs half a head apart.  A 480P block (4680 tokens, 12 + 12 heads of 128 dims, bf16): 22 us, 3.9
+// TB/s, and 6 for the second launch; 4099 tokens of 16 + 4 heads in 32 bits, positions given, 28 us, 4.5 TB/s, and 4.
 // ---------------------------------------------------------------------------
 
 template <typename XT, typename OT, bool HALVES>

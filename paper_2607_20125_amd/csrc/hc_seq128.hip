@@ -32,6 +32,13 @@ using namespace dev;
 // 480P block over its 4-bit window 0.83-0.90 ms, 1.05-1.14 PFLOP/s: conversions and their LDS
 // writes take the issue slots that a step has left (58% busy), so a tile takes 27% more cycles than a packed one.
 // Copies of the next tiles behind a branch instead of a rule for whole steps: 3.5% slower.
+//
+// With a window, or pages: written-out steps run over the whole tiles among the first tokens, and over those of the window;
+// single steps, masked where they have to be, before, between and behind them.  (One nested loop over both kept more alive
+// than the registers hold: 1.50 ms instead of 1.08.)  Pages: each copy is of a run of 16 rows, whose place comes by a scalar load a tile
+// ahead.  A clip of four 480P blocks, window of two blocks and the first: 1.05 ms, 1.15 PFLOP/s, cores busy 66%; five prompts' 2500 rows
+// over pages of 32, window 4096, 8 x 4 heads: 167-186 us, 0.8-0.9 PFLOP/s, cores busy 47%: masked steps at
+// both ends of a window, and 968 work groups of uneven length on 512 places.
 // ---------------------------------------------------------------------------
 constexpr int kPre = 6;      // pairs of the next tile formed during PV
 constexpr int kAhead = 3;    // operand reads in flight

@@ -260,9 +260,10 @@ hc_status grad_plan(hc_ctx *c, const hc_window_grad_args *g, GradArgs &a) {
   const int64_t k_tiles = unit_room(p->n_keys, p->n_seqs, 1, kGradKeys, alike);
   const int64_t units = k_tiles * p->n_kv_heads;
   // Key units are cut into pieces of rows until 512 work groups run (two for each CU with 64-dim heads, two rounds with 128), but
-  // no piece is shorter than 4 tiles of rows: a partial gradient costs two writes, two reads and a launch.  512, 768 and 1024: one
-  // sequence of 2048, 4 x 4 heads of 128 dims 118, 136 and 150 us; two heads of 4096, 64 dims 87, 95 and 103; six prompts of up to
-  // 1450, window 512, 4 x 3 heads of 64 dims 77, 74 and 72 (256: 122, 89 and 125).
+  // no piece is shorter than 4 tiles of rows: a partial gradient costs two writes, two reads and a launch.  Forward and gradients
+  // with 256, 384, 512 and 768: one sequence of 2048, 4 x 4 heads of 128 dims 152, 154, 159 and 175 us; two heads of 4096, 64 dims
+  // 104, 100, 106 and 114; six prompts of up to 1450, window 512, 4 x 3 heads of 64 dims 126, 94, 85 and 90; ten of up to 2000,
+  // window 1000, 2 x 4 heads 139, 117, 119 and 120.
   int64_t queries = (int64_t)p->n_tokens / p->n_seqs;            // that see a key, about
   if (p->window > 0) queries = std::min(queries, (int64_t)p->window + p->causal_block + kGradKeys);
   const int64_t tiles = queries * a.seq.group / 64;

@@ -56,7 +56,7 @@ struct GradArgs {
   const float *lse;              // [heads][n_tokens]
   uint16_t *dq, *dk, *dv;
   int64_t do_token, do_head, dq_token, dq_head, dk_token, dk_head, dv_token, dv_head;
-  float *stats;                  // [2][heads][n_tokens]: lse in log2 units, sum over dims of dout * o
+  float *stats;                  // [2][heads][n_tokens]: -lse / scale, -(sum over dims of dout * o)
   int32_t key_tiles;             // key units that the launch has room for
   float scale;
   // key units are cut into pieces of rows, whose partial gradients a further launch adds up in order
