@@ -681,16 +681,16 @@ __device__ __forceinline__ void queries_unit(const GradArgs &a, int block, Share
 }
 
 // Both in one launch, units of keys first, which are the longer ones: neither needs the other, and the last of the ones run beside
-// the first of the others.  (Forward and gradients, two launches and one: six prompts, window 512, 64 dims 104 and 84 us; two 480P
-// blocks, 12 heads of 128 dims 1760 and 1661; 6000 tokens, 4 x 4 heads, causal 719 and 700; three 480P blocks, where power sets
-// the pace, 2744 and 2783.)  Under a causal mask early keys and late queries have most to do, so that queries come from the
-// last on (that clip: 2766 us instead of 2841).
+// the first of the others.  (Forward and gradients, two launches and one: six prompts, window 512, 64 dims 104 and 81 us; two 480P
+// blocks, 12 heads of 128 dims 1760 and 1630; 6000 tokens, 4 x 4 heads, causal 719 and 650; three 480P blocks, where power sets
+// the pace, 2744 and 2728.)  Early keys and late queries, which have most to do under a causal mask, come first among their own
+// (see seq_unit; queries from the first on: 650 -> 691, 2728 -> 2747).
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void grad_kernel(GradArgs a) {
   __shared__ Shared<D> lds;
   const int keys = a.key_tiles * a.seq.kv_heads * a.n_split, block = (int)blockIdx.x;
   if (block < keys) keys_unit<D>(a, block, lds);
-  else queries_unit<D>(a, (int)gridDim.x - 1 - block, lds);
+  else queries_unit<D>(a, block - keys, lds);
 }
 
 template <int D>
