@@ -453,7 +453,7 @@ hc_status hc_qcache_attention(hc_ctx *ctx, const hc_qcache *cache,
 
 /* Root-mean-square norm of every head, then the rotation of hc_rotate:
  * y = R (x r w), r = (mean of x^2 over the head's dims + eps)^(-1/2), in 32 bits, rounded once to the output's
- * type (squares overflow 32 bits from 1.8e19 on).  All dims are normed; those behind the rotated ones are
+ * type (squares overflow 32 bits from 1.8e19 on; with eps = 0 a head of zeros, or of values below 1e-19, has no norm).  All dims are normed; those behind the rotated ones are
  * not turned.  In place as hc_rotate. */
 typedef struct {
   const void *x;             /* [n_tokens][n_heads][head_dim] by the strides below       */
@@ -559,8 +559,8 @@ typedef struct {
 hc_status hc_window_workspace(hc_ctx *ctx, const hc_window_args *args, int64_t *bytes);
 hc_status hc_window_attention(hc_ctx *ctx, const hc_window_args *args, hc_stream stream);
 
-/* Its gradients.  `forward` holds the forward call's q, k, v, out and lse (all only read here) and sizes; its
- * workspace is not used.  With p the probabilities and s the scale,
+/* Its gradients.  `forward` holds the forward call's q, k, v, out (not in q's place) and lse, all only read here, and
+ * sizes; its workspace is not used.  With p the probabilities and s the scale,
  *   dv = p^T dout,  ds = p (dout v^T - rowsum(dout out)) s,  dq = ds k,  dk = ds^T q,
  * summed over the query heads that share a key head.  p and ds are rounded to bfloat16 for the products, sums are
  * float32, rounded once; repeated calls agree bit for bit.  Token strides of q, k, v and dout are below 2^24, a given

@@ -471,6 +471,7 @@ hc_status hc_window_attention_backward(hc_ctx *c, const hc_window_grad_args *g, 
     if (st == HC_OK) st = check_tensor(c, {"dout", g->dout, g->dout_token, g->dout_head, p.n_tokens, p.n_heads});
     if (st == HC_OK) st = check_output(c, {"dq", g->dq, g->dq_token, g->dq_head, p.n_tokens, p.n_heads}, p.head_dim);
     if (st == HC_OK && !p.lse) st = fail(c, HC_E_INVAL, "lse is NULL");
+    if (st == HC_OK && p.q == p.out) st = fail(c, HC_E_INVAL, "the forward call's out has overwritten q");
   }
   if (st == HC_OK && p.n_keys > 0) {
     st = check_tensor(c, {"k", p.k, p.k_token, p.k_head, p.n_keys, p.n_kv_heads});

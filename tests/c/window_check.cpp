@@ -327,7 +327,7 @@ void window_refusals() {
     }, call);
   refuses<G>(x.c, good_window(), {[](G &g) { g.forward.out_head = 56; }, [](G &g) { g.forward.out_token = 0; }}, forward);
   refuses<G>(x.c, good_window(), {
-      [](G &g) { g.forward.lse = nullptr; }, [](G &g) { g.dout = nullptr; }, [](G &g) { g.dout_token = 100; },
+      [](G &g) { g.forward.lse = nullptr; }, [](G &g) { g.forward.out = at; }, [](G &g) { g.dout = nullptr; }, [](G &g) { g.dout_token = 100; },
       [](G &g) { g.dq = memory + 4; }, [](G &g) { g.dk = nullptr; }, [](G &g) { g.dv = nullptr; }, [](G &g) { g.dq_token = 0; },
       [](G &g) { g.dk_head = 56; }, [](G &g) { g.dv_token = 64; }, [](G &g) { g.workspace = nullptr; }, [](G &g) { g.workspace_bytes = 10; },
       [](G &g) { g.workspace = memory + 4; }, [](G &g) { g.forward.q_token = 1 << 24; }, [](G &g) { g.forward.v_token = 1 << 24; },

@@ -431,3 +431,46 @@ def test_rows_behind_32_bit_offsets(ctx, dim):
     a, ta, b, tb = W.norm_rotate_backward(q, w, do, pos, (dim,))
     W.assert_close(dx, a, ta, "dx")
     W.assert_close(dw, b, tb, "dw")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_key_head_of_many(ctx, dim):
+    """More query heads on a key head than a unit has rows."""
+    for group, queries, keys in ((150, [3, 20], [40, 20]), (300, [1], [70])):
+        q, k, v, do = (normal(680 + i, sum(n), h, dim) for i, (n, h) in enumerate(((queries, group), (keys, 1), (keys, 1), (queries, group))))
+        d = [t.cuda() for t in (q, k, v, do)]
+        cu = offsets(queries), offsets(keys)
+        lse = torch.empty(group, sum(queries), device="cuda")
+        out = ctx.window_attention(*d[:3], *cu, lse=lse, window=17, sinks=2)
+        grads = ctx.window_attention_backward(*d[:3], out, lse, d[3], *cu, window=17, sinks=2)
+        pages, table = new_pages(ctx, 20, 16, 1, dim), random_table(13, len(keys), 5, 20).cuda()
+        ctx.paged_append(pages, table, d[1], d[2], ints([0] * len(keys)), cu[1])
+        paged = ctx.paged_attention(pages, table, d[0], ints(keys), cu[0], window=17, sinks=2)
+        a = b = 0
+        for n, m in zip(queries, keys):
+            qs, ks, vs, dos = q[a:a + n], k[b:b + m], v[b:b + m], do[a:a + n]
+            seen = W.sees(n, m, 1, 17, 2)
+            want, mag, _, _ = W.attention(qs, ks, vs, seen)
+            W.assert_attention(out[a:a + n], want, mag, "out")
+            W.assert_attention(paged[a:a + n], want, mag, "pages")
+            for t, (name, (g, tol)) in zip(grads, W.gradients(qs, ks, vs, dos, seen).items()):
+                lo, hi = (a, a + n) if name == "dq" else (b, b + m)
+                W.assert_close(t[lo:hi], g, tol, name)
+            a, b = a + n, b + m
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scales(ctx, dim):
+    """A scale of the caller's, small and large."""
+    n = 150
+    q, k, v, do = (normal(690 + i, n, 2, dim) for i in range(4))
+    d = [t.cuda() for t in (q, k, v, do)]
+    seen = W.sees(n, n, 1, 60, 1)
+    for scale in (1e-20, 0.01, 0.6):
+        lse = torch.empty(2, n, device="cuda")
+        kw = dict(window=60, sinks=1, softmax_scale=scale)
+        out = ctx.window_attention(*d[:3], lse=lse, **kw)
+        W.assert_attention(out, *W.attention(q, k, v, seen, scale)[:2], f"scale {scale}")
+        grads = ctx.window_attention_backward(*d[:3], out, lse, d[3], **kw)
+        for t, (name, (g, tol)) in zip(grads, W.gradients(q, k, v, do, seen, scale).items()):
+            W.assert_close(t, g, tol, f"{name}, scale {scale}")
