@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormArgs a) {
 // by the launch's work groups, adding dw up in registers; a work group's sums, joined in LDS, go to one row of the
 // workspace, and a second launch adds those rows up in a fixed order, so that results repeat bit for bit.  Two heads in
 // flight, or one with pairs half a head apart.  A 480P block (4680 tokens, 12 + 12 heads of 128 dims, bf16): 22 us, 3.9
-// TB/s, and 6 for the second launch; 4099 tokens of 16 + 4 heads in 32 bits, positions given, 28 us, 4.5 TB/s, and 4.
+// TB/s, and 4 for the second launch; 4099 tokens of 16 + 4 heads in 32 bits, positions given, 28 us, 4.5 TB/s, and 4.
 // ---------------------------------------------------------------------------
 
 template <typename XT, typename OT, bool HALVES>
@@ -226,21 +226,30 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_backward_kernel(NormArgs
   a.part[(first + (int64_t)s.cut * a.groups + blockIdx.x) * r.head_dim + threadIdx.x] = sum;
 }
 
-// dw of 8 dims of a tensor: 32 threads a dim add every 32nd row, and are joined in LDS.
-__global__ __launch_bounds__(kThreads) void norm_weights_kernel(NormArgs a) {
-  __shared__ float sw[kThreads];
+// dw of 8 dims of a tensor: 128 threads a dim add every 128th row, and are joined in LDS, 16 and then 8 of them.  (With 32 threads a
+// dim: a 480P block's gradients from memory 33.4 us instead of 31.6.)
+constexpr int kWeightThreads = 1024;
+__global__ __launch_bounds__(kWeightThreads) void norm_weights_kernel(NormArgs a) {
+  constexpr int each = kWeightThreads / 8;
+  __shared__ float sw[kWeightThreads], half[64];
   const NormTensor &t = a.t[blockIdx.y];
   if (!t.dweight) return;
   const int d = threadIdx.x % 8, first = threadIdx.x / 8, dim = blockIdx.x * 8 + d;
   const int64_t rows = norm_parts(a, blockIdx.y);
   const float *p = a.part + (blockIdx.y ? norm_parts(a, 0) : 0) * a.rotate.head_dim + dim;
   float sum = 0.f;
-#pragma unroll 16
-  for (int64_t i = first; i < rows; i += 32) sum += p[i * a.rotate.head_dim];
+#pragma unroll 8
+  for (int64_t i = first; i < rows; i += each) sum += p[i * a.rotate.head_dim];
   sw[threadIdx.x] = sum;
   __syncthreads();
+  if (first < 8) {
+    sum = 0.f;
+    for (int i = 0; i < each / 8; ++i) sum += sw[(first * (each / 8) + i) * 8 + d];
+    half[threadIdx.x] = sum;
+  }
+  __syncthreads();
   if (first) return;
-  for (int i = 1; i < 32; ++i) sum += sw[i * 8 + d];
+  for (int i = 1; i < 8; ++i) sum += half[i * 8 + d];
   t.dweight[dim] = sum;
 }
 
@@ -266,7 +275,7 @@ hipError_t launch_norm_backward(const NormArgs &a, int x_type, int out_type, boo
   if (a.groups > 0) { HC_NORM_TYPES(norm_rotate_backward_kernel) }
   const bool weights = a.t[0].dweight || (a.n_tensors > 1 && a.t[1].dweight);
   if (weights)
-    hipLaunchKernelGGL(norm_weights_kernel, dim3((uint32_t)(a.rotate.head_dim / 8), (uint32_t)a.n_tensors), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(norm_weights_kernel, dim3((uint32_t)(a.rotate.head_dim / 8), (uint32_t)a.n_tensors), dim3(kWeightThreads), 0, s, a);
   return hipGetLastError();
 }
 #undef HC_NORM_HALVES
