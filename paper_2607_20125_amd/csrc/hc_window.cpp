@@ -172,13 +172,17 @@ hc_status paged_plan(hc_ctx *c, const hc_pages *pages, const hc_page_table *tabl
   // (the kernel for few rows reads the cache once per 16 rows: see cached_plan in hc_ops.cpp)
   few_rows = rows <= (int64_t)a.n_seqs * 2 * kDecodeRows;
   const int R = few_rows ? kDecodeRows : kSeqRows;
-  const int64_t tiles = unit_room(p->n_tokens, a.n_seqs, a.group, R, p->cu_seqlens == nullptr);
+  // (a token adds ceil(group / R) units at most: no more are made room for where each sequence has one)
+  const int64_t tiles = std::min(unit_room(p->n_tokens, a.n_seqs, a.group, R, p->cu_seqlens == nullptr),
+                                 (int64_t)p->n_tokens * ((a.group + R - 1) / R));
   if (rows > INT32_MAX - kSeqRows || !good_grid(tiles * a.kv_heads))
     return fail(c, HC_E_INVAL, "too many query rows for one call");
   a.tiles = (int)tiles;
   const int64_t keys = seen_at_most(a, p->max_kv > 0 ? std::min(p->max_kv, a.capacity) : a.capacity, R);
   const int64_t units = seq_units(a);
-  if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units < 192 ? 1024 : 1536, 4, kDecodeMaxSplit);
+  // Work groups wanted for few rows: 1024 against 1536, single tokens: 48 sequences of up to 8192 keys, 4 x 7 heads of 64 dims (192
+  // units) 24.3 and 27.7 us; 32 of up to 4096, 8 x 4 heads of 128 dims (256) 64 and 67; 24 of up to 5000, 12 heads (288) 91.8 and 89.7.
+  if (few_rows) choose_split(a, keys, units < 64 || units >= 512 ? 512 : units <= 256 ? 1024 : 1536, 4, kDecodeMaxSplit);
   else choose_split(a, keys, 512, 8, kSeqMaxSplit);
   // (the wide kernel's copies hold offsets of a run of 16 rows in 32 bits)
   a.wide = pages->head_dim == 128 && !few_rows && a.k_token < 1 << 24 && a.v_token < 1 << 24 && wide_rows(a, keys);
