@@ -30,11 +30,11 @@ using namespace dev;
 // 8 g .. 8 g + 7 of every 16 (see hc_device.h), in the order that the second products contract.
 //
 // Bound by the matrix cores and the power that they draw with 128-dim heads: forward and gradients of a clip of three 480P blocks (14040
-// tokens, 12 heads, a block sees itself and the first) 2.77 ms, the gradients 2.1-2.2 ms of it, 1.05-1.1 PFLOP/s of the 7 products, cores busy 52%
-// at 1.9 to 2.0 GHz.  One wave on a SIMD, so that an operand and all sums stay in its 512 registers; two waves, with half of
+// tokens, 12 heads, a block sees itself and the first) 2.77 ms, the gradients 2.1-2.2 ms of it, 1.05-1.1 PFLOP/s of the 7 products, cores busy 53%
+// at 2.0 GHz.  One wave on a SIMD, so that an operand and all sums stay in its 512 registers; two waves, with half of
 // them, took 7% longer, and left no room for operands that are read 7 products ahead.  Without its copies a step would be 11%
 // faster, without vector instructions 16%, without LDS reads 10% (timed apart).  64-dim heads: two waves on a SIMD; six prompts of
-// 4000 tokens together (4 x 3 heads, window 512) 48 us, cores busy 24%: exponentials, masks and products of a wave in turn, and
+// 4000 tokens together (4 x 3 heads, window 512) 45 us, cores busy 26%: exponentials, masks and products of a wave in turn, and
 // 1.5 waves on a SIMD at the mean.
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kTile = 64;        // streamed rows of a tile
