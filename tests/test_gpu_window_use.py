@@ -474,3 +474,43 @@ def test_scales(ctx, dim):
         grads = ctx.window_attention_backward(*d[:3], out, lse, d[3], **kw)
         for t, (name, (g, tol)) in zip(grads, W.gradients(q, k, v, do, seen, scale).items()):
             W.assert_close(t, g, tol, f"{name}, scale {scale}")
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("queries,keys", [(1, 700), (40, 3000), (300, 1500), (5, 20000)])
+def test_logarithms_of_merged_ranges(ctx, dim, queries, keys):
+    """Few rows over many keys are cut into ranges: the logarithms of the whole rows, and gradients from them."""
+    q, k, v, do = (normal(700 + i, n, h, dim) for i, (n, h) in enumerate(((queries, 4), (keys, 2), (keys, 2), (queries, 4))))
+    d = [t.cuda() for t in (q, k, v, do)]
+    cu = offsets([queries]), offsets([keys])
+    for window, sinks in ((0, 0), (keys // 2, 100)):
+        seen = W.sees(queries, keys, 1, window, sinks)
+        lse = torch.full((4, queries), math.nan, device="cuda")
+        kw = dict(window=window, sinks=sinks)
+        out = ctx.window_attention(*d[:3], *cu, lse=lse, **kw)
+        want, mag, logs, _ = W.attention(q, k, v, seen)
+        W.assert_attention(out, want, mag, "out")
+        assert bool(((lse.cpu().double() - logs).abs() <= 2.0 ** -8 * 1.02).all())
+        grads = ctx.window_attention_backward(*d[:3], out, lse, d[3], *cu, **kw)
+        for t, (name, (g, tol)) in zip(grads, W.gradients(q, k, v, do, seen).items()):
+            W.assert_close(t, g, tol, name)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_gradients_of_large_logits(ctx, dim):
+    """Logits of several hundreds: rows that a few keys carry, and whose logarithms are large.
+
+    Forming p again, a logit is off by 2^-24 of the sum of its products' magnitudes for each of the up to 8 products
+    along its dims, the logarithm by as much once more: 2^-20 of that sum in all, which scales every tolerance's 2^-7."""
+    n = 420
+    q, k = (normal(720 + i, n, 2, dim, spread=8.0) for i in range(2))
+    v, do = (normal(722 + i, n, 2, dim) for i in range(2))
+    d = [t.cuda() for t in (q, k, v, do)]
+    for window, sinks in ((0, 0), (90, 6)):
+        seen = W.sees(n, n, 1, window, sinks)
+        size = float((q.double().abs().transpose(0, 1) @ k.double().abs().permute(1, 2, 0)).max()) * dim ** -0.5
+        lse = torch.empty(2, n, device="cuda")
+        out = ctx.window_attention(*d[:3], lse=lse, window=window, sinks=sinks)
+        grads = ctx.window_attention_backward(*d[:3], out, lse, d[3], window=window, sinks=sinks)
+        for t, (name, (g, tol)) in zip(grads, W.gradients(q, k, v, do, seen).items()):
+            W.assert_close(t, g, tol * (1 + size * 2.0 ** -20 / 2.0 ** -7), name)
