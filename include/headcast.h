@@ -540,8 +540,8 @@ hc_status hc_paged_attention(hc_ctx *ctx, const hc_pages *pages, const hc_page_t
 
 /* Attention over packed sequences, as hc_packed_attention, with the mask above.  `lse`, if not NULL, gets the
  * logarithm of every row's sum of exponentials, which hc_window_attention_backward takes: float32
- * [n_heads][n_tokens], -infinity for a query that sees nothing (the sum is of the probabilities as rounded to
- * bfloat16, so it is off by up to 2^-8). */
+ * [n_heads][n_tokens], -infinity for a query that sees nothing.  Its sum is of the probabilities in 32 bits, not of the
+ * rounded ones that weigh the values. */
 typedef struct {
   const void *q, *k, *v;     /* bf16 [tokens][heads][head_dim] by the strides below       */
   void *out;                 /* bf16 [n_tokens][n_heads][head_dim]; may be q itself with

@@ -132,8 +132,8 @@ inline hc_status check_workspace(hc_ctx *c, const void *p, int64_t bytes, int64_
   return HC_OK;
 }
 
-inline int64_t part_bytes(const SeqArgs &a, int head_dim, int rows) {
-  return seq_cut_units(a) * (16 + a.n_split * seq_part_floats(rows, head_dim) * 4);
+inline int64_t part_bytes(const SeqArgs &a, int head_dim, int rows, bool logs = false) {
+  return seq_cut_units(a) * (16 + a.n_split * seq_part_floats(rows, head_dim, logs) * 4);
 }
 
 inline void use_workspace(SeqArgs &a, void *p) {

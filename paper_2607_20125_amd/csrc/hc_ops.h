@@ -80,7 +80,7 @@ struct SeqArgs {
   // into n_split key ranges, whose work groups come after those.
   int32_t whole, n_split;
   int32_t *head;                 // cut units: [unit - whole][4]: q0, row0, rows (0: no such unit)
-  float *part;                   // [unit - whole][n_split][rows (d + 2)]
+  float *part;                   // [unit - whole][n_split][seq_part_floats]
   float scale_log2;              // softmax scale * log2(e)
   bool wide;                     // 128-dim heads: waves of 64 rows (hc_seq128.hip)
   // attention with a window (hc_window.cpp)
@@ -94,8 +94,9 @@ struct SeqArgs {
 inline int64_t seq_units(const SeqArgs &a) { return (int64_t)a.tiles * a.kv_heads; }
 inline int64_t seq_cut_units(const SeqArgs &a) { return a.n_split > 1 ? seq_units(a) - a.whole : 0; }
 inline int64_t seq_groups(const SeqArgs &a) { return a.whole + (seq_units(a) - a.whole) * a.n_split; }
-// Floats of one partial result: rows of d sums, then the rows' maxima and sums.
-constexpr int64_t seq_part_floats(int rows, int d) { return (int64_t)rows * (d + 2); }
+// Floats of one partial result: rows of d sums, then the rows' maxima and sums, and where logarithms are asked for the
+// sums of the probabilities before their rounding.
+constexpr int64_t seq_part_floats(int rows, int d, bool logs = false) { return (int64_t)rows * (d + (logs ? 3 : 2)); }
 hipError_t launch_seq(const SeqArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_seq128(const SeqArgs &a, hipStream_t s);
 hipError_t launch_decode(const SeqArgs &a, int head_dim, hipStream_t s);

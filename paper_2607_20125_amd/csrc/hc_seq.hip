@@ -29,10 +29,14 @@ using namespace dev;
 // 16 keys at a time; a run without a page has values of zero and logits of -infinity.  Six prompts of 4000 tokens together
 // (window 512, 4 x 3 heads of 64 dims): 26 us, ten tiles a unit on 1.1 waves a SIMD, 2.4 us each.  (Cut into
 // ranges for more waves, partial results and their merge cost what it gains: 31 us.)
+//
+// LOGS: the logarithms of the row sums too.  Outputs are divided by the sum of the rounded probabilities, which are what was
+// multiplied, but that sum is off by up to 2^-9, and a logarithm of it would be as well; its own sum is of the
+// probabilities in 32 bits.
 // ---------------------------------------------------------------------------
 constexpr int kWaves = kSeqRows / 32;
 
-template <int D, Keys SRC>
+template <int D, Keys SRC, bool LOGS = false>
 __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(SeqArgs a) {
   constexpr bool QUANT = SRC == Keys::kQuant, PAGED = SRC == Keys::kPaged, WINDOW = PAGED || SRC == Keys::kWindow;
   constexpr int KT = kSeqKeys, NKK = D / 16, NDB = D / 32, TILE = KT * D;
@@ -235,7 +239,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
   f32x16 acc[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) acc[db] = f32x16{};
-  float m_run = kMInit, l_run = 0.f;
+  float m_run = kMInit, l_run = 0.f, e_run = 0.f;      // (e_run: LOGS)
   if (t0 < t1) {
     if constexpr (PAGED) entries = page_entry(a, u, tiles.place(t0), lane);
     load(t0);
@@ -283,6 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;
+      e_run *= alpha;
 #pragma unroll
       for (int db = 0; db < NDB; ++db) acc[db] *= alpha;
     }
@@ -292,12 +297,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          pf[kb][h][e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[kb][8 * h + e], sl2, -m_run));
+        for (int e = 0; e < 8; e += 2) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * h + e], sl2, -m_run));
+          const float y = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * h + e + 1], sl2, -m_run));
+          pf[kb][h][e] = (__bf16)x;
+          pf[kb][h][e + 1] = (__bf16)y;
+          if constexpr (LOGS) e_run += x + y;
+        }
+        // (here, or the compiler adds a tile's probabilities behind it all and keeps them until then: 53 registers spilled)
         const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
         for (int e = 0; e < 8; e += 2)
           l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{pf[kb][h][e], pf[kb][h][e + 1]}, one, l_run, false);
+        // (here, or the compiler adds a tile's probabilities behind all products and keeps them until then: 53 registers spilled)
+        if constexpr (LOGS) asm volatile("" : "+v"(e_run), "+v"(l_run));
       }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -328,11 +341,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
         out.put(n, 8 * db + 2 * rq + g, acc[db][4 * rq] * inv, acc[db][4 * rq + 1] * inv, acc[db][4 * rq + 2] * inv,
                 acc[db][4 * rq + 3] * inv);
     out.store(a, u, head, wave * 32, lane);
-    if constexpr (WINDOW)
-      if (a.lse && g == 0 && row < u.rows) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run, l_tot);
+    if constexpr (LOGS) {
+      const float e_tot = sum_xor32(e_run);
+      if (g == 0 && row < u.rows) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run, e_tot);
+    }
   } else {
     const int lrow = wave * 32 + n;
-    float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
+    float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D, LOGS);
+    const float e_tot = LOGS ? sum_xor32(e_run) : 0.f;
     float *op = pp + (int64_t)lrow * D;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -343,6 +359,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
     if (g == 0) {
       pp[kSeqRows * D + lrow] = m_run;
       pp[kSeqRows * D + kSeqRows + lrow] = l_tot;
+      if constexpr (LOGS) pp[kSeqRows * D + 2 * kSeqRows + lrow] = e_tot;
     }
   }
 }
@@ -350,9 +367,11 @@ __global__ __launch_bounds__(64 * kWaves, D == 64 ? 3 : 2) void seq_attn_kernel(
 // ---------------------------------------------------------------------------
 // Merge of the n_split partial results of every unit: O = sum_i 2^(m_i - M) acc_i /
 // sum_i 2^(m_i - M) l_i.  A thread takes 4 dims of a row; a work group 256 * 4 / D rows.
+// LOGS: and the logarithm of the sum of the ranges' sums in 32 bits.
 // ---------------------------------------------------------------------------
-template <int D, int R>
+template <int D, int R, bool LOGS>
 __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
+  constexpr int64_t PART = seq_part_floats(R, D, LOGS);
   constexpr int TR = D / 4, RW = 256 / TR, RP = R / RW;      // threads a row, rows a group, groups a unit
   static_assert(R % RW == 0, "rows of a unit");
   const int unit = blockIdx.x / RP;
@@ -362,15 +381,16 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   const int lrow = (blockIdx.x % RP) * RW + threadIdx.x / TR, row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int dim = threadIdx.x % TR * 4;
-  const float *pp = a.part + (int64_t)unit * a.n_split * seq_part_floats(R, D);
+  const float *pp = a.part + (int64_t)unit * a.n_split * PART;
   float M = kMInit;
-  for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, pp[i * seq_part_floats(R, D) + R * D + lrow]);
+  for (int i = 0; i < a.n_split; ++i) M = fmaxf(M, pp[i * PART + R * D + lrow]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
+  float l = 0.f, sum = 0.f;
   for (int i = 0; i < a.n_split; ++i) {
-    const float *p = pp + i * seq_part_floats(R, D);
+    const float *p = pp + i * PART;
     const float w = __builtin_amdgcn_exp2f(p[R * D + lrow] - M);
     l += w * p[R * D + R + lrow];
+    if constexpr (LOGS) sum += w * p[R * D + 2 * R + lrow];
     o += w * *reinterpret_cast<const f32x4 *>(p + lrow * D + dim);
   }
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
@@ -380,16 +400,18 @@ __global__ __launch_bounds__(256) void seq_merge_kernel(SeqArgs a) {
   w.x = __builtin_bit_cast(uint32_t, x);
   w.y = __builtin_bit_cast(uint32_t, y);
   *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = w;
-  if (a.lse && dim == 0) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, l);
+  if constexpr (LOGS)
+    if (dim == 0) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, sum);
 }
 
 // The same for many partial results: a work group takes one row, its threads 4 dims of every
 // 256 * 4 / D-th of them, so that their reads are in flight together.  (One thread summing all 128
 // of a long cache's row took 66 us beside an attention kernel of 29.)
-template <int D, int R>
+template <int D, int R, bool LOGS>
 __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
+  constexpr int64_t PART = seq_part_floats(R, D, LOGS);
   constexpr int TR = D / 4, NG = 256 / TR;
-  __shared__ float sW[kDecodeMaxSplit], sL[kDecodeMaxSplit], sO[NG][D], sM[4];
+  __shared__ float sW[kDecodeMaxSplit], sL[kDecodeMaxSplit], sO[NG][D], sM[4], sE[LOGS ? kDecodeMaxSplit : 1];
   const int unit = blockIdx.x / R, lrow = blockIdx.x % R;
   SeqUnit u;
   int head;
@@ -397,8 +419,8 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   const int row = u.row0 + lrow;
   if (row >= u.rows) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float *pp = a.part + (int64_t)unit * a.n_split * seq_part_floats(R, D);
-  const float *ml = pp + tid * seq_part_floats(R, D) + R * D + lrow;
+  const float *pp = a.part + (int64_t)unit * a.n_split * PART;
+  const float *ml = pp + tid * PART + R * D + lrow;
   const float m = tid < a.n_split ? ml[0] : kMInit;
   const float l = tid < a.n_split ? ml[R] : 0.f;
   float M = m;
@@ -410,13 +432,14 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   const float w = __builtin_amdgcn_exp2f(m - M);
   sW[tid] = w;
   sL[tid] = w * l;
+  if constexpr (LOGS) sE[tid] = tid < a.n_split ? w * ml[2 * R] : 0.f;
   __syncthreads();
   const int grp = tid / TR, dim = tid % TR * 4;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   const float *op = pp + lrow * D + dim;
 #pragma unroll 4
   for (int i = grp; i < a.n_split; i += NG)
-    o += sW[i] * *reinterpret_cast<const f32x4 *>(op + i * seq_part_floats(R, D));
+    o += sW[i] * *reinterpret_cast<const f32x4 *>(op + i * PART);
   *reinterpret_cast<f32x4 *>(&sO[grp][dim]) = o;
   __syncthreads();
   if (tid >= TR) return;
@@ -431,7 +454,12 @@ __global__ __launch_bounds__(256) void seq_merge_many_kernel(SeqArgs a) {
   r.x = __builtin_bit_cast(uint32_t, x);
   r.y = __builtin_bit_cast(uint32_t, y);
   *reinterpret_cast<uint2 *>(a.o + (u.q0 + qi) * a.o_token + qh * a.o_head + dim) = r;
-  if (a.lse && dim == 0) a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, total);
+  if constexpr (LOGS)
+    if (dim == 0) {
+      float sum = 0.f;
+      for (int i = 0; i < a.n_split; ++i) sum += sE[i];
+      a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(M, sum);
+    }
 }
 
 }  // namespace
@@ -454,9 +482,11 @@ hipError_t launch_window(const SeqArgs &a, int head_dim, hipStream_t s) {
   const dim3 grid((uint32_t)seq_groups(a)), block(64 * kWaves);
   if (head_dim == 128) {
     if (a.table) hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kPaged>), grid, block, 0, s, a);
+    else if (a.lse) hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kWindow, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((seq_attn_kernel<128, Keys::kWindow>), grid, block, 0, s, a);
   } else {
     if (a.table) hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kPaged>), grid, block, 0, s, a);
+    else if (a.lse) hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kWindow, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((seq_attn_kernel<64, Keys::kWindow>), grid, block, 0, s, a);
   }
   return hipGetLastError();
@@ -466,15 +496,17 @@ hipError_t launch_seq_merge(const SeqArgs &a, int head_dim, int rows, hipStream_
   const bool many = a.n_split > 8;
   const int per = many ? rows : rows * head_dim / 1024;      // work groups of a unit
   const dim3 grid((uint32_t)(seq_cut_units(a) * per)), block(256);
-#define HC_MERGE(D, R)                                                                     \
-  if (many) hipLaunchKernelGGL((seq_merge_many_kernel<D, R>), grid, block, 0, s, a);       \
-  else hipLaunchKernelGGL((seq_merge_kernel<D, R>), grid, block, 0, s, a)
+#define HC_MERGE(D, R, LOGS)                                                                     \
+  if (many) hipLaunchKernelGGL((seq_merge_many_kernel<D, R, LOGS>), grid, block, 0, s, a);       \
+  else hipLaunchKernelGGL((seq_merge_kernel<D, R, LOGS>), grid, block, 0, s, a)
   if (head_dim == 128) {
-    if (rows == kSeqRows) { HC_MERGE(128, kSeqRows); }
-    else { HC_MERGE(128, kDecodeRows); }
+    if (a.lse) { HC_MERGE(128, kSeqRows, true); }
+    else if (rows == kSeqRows) { HC_MERGE(128, kSeqRows, false); }
+    else { HC_MERGE(128, kDecodeRows, false); }
   } else {
-    if (rows == kSeqRows) { HC_MERGE(64, kSeqRows); }
-    else { HC_MERGE(64, kDecodeRows); }
+    if (a.lse) { HC_MERGE(64, kSeqRows, true); }
+    else if (rows == kSeqRows) { HC_MERGE(64, kSeqRows, false); }
+    else { HC_MERGE(64, kDecodeRows, false); }
   }
 #undef HC_MERGE
   return hipGetLastError();

@@ -95,7 +95,8 @@ __device__ __forceinline__ const uint16_t *uniform_ptr(const uint16_t *p) {
   return (const uint16_t *)((uint64_t)hi << 32 | lo);
 }
 
-template <Keys SRC>
+// LOGS: the logarithms of the row sums too (see hc_seq.hip).
+template <Keys SRC, bool LOGS = false>
 __device__ __forceinline__ void attend128(const SeqArgs &a) {
   constexpr bool QUANT = SRC == Keys::kQuant, PAGED = SRC == Keys::kPaged, WINDOW = PAGED || SRC == Keys::kWindow;
   constexpr int D = 128, NQB = 2, KT = kSeqKeys, NKK = D / 16, NDB = D / 32;
@@ -503,10 +504,12 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
   auto score = [](const Scores &s, int p, int e) {
     return s[p / 16][(p / 4) % 2][8 * ((p / 8) % 2) + 2 * (p % 4) + e];
   };
+  float e_run[NQB] = {};          // LOGS: this lane's half of its rows' sums
   auto pack = [&](Probs &pf, int p, float x0, float x1) {
     uint32_t r;
     asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(x0), "v"(x1));
     pf[p / 8][(p / 4) % 2][p % 4] = r;
+    if constexpr (LOGS) e_run[(p / 4) % 2] += x0 + x1;
   };
   auto probs = [](const Probs &pf, int chunk, int qb) { return __builtin_bit_cast(bf16x8, pf[chunk][qb]); };
   auto row_sums = [&](const Probs &pf, int chunk) {
@@ -757,6 +760,7 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
       for (int db = 0; db < NDB; ++db) acc[qb][db] = f32x16{};
       m_run[qb] = kMInit;
       l_run[qb] = 0.f;
+      e_run[qb] = 0.f;
     }
     __syncthreads();              // every wave is done with the slots
     // (an absent run's rows are copied from page 0 and do not count)
@@ -804,6 +808,7 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
           const float alpha = __builtin_amdgcn_exp2f(m_run[qb] - m_new);
           m_run[qb] = m_new;
           l_run[qb] *= alpha;
+          e_run[qb] *= alpha;
 #pragma unroll
           for (int db = 0; db < NDB; ++db) acc[qb][db] *= alpha;
         }
@@ -811,8 +816,10 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
 #pragma unroll
       for (int p = 0; p < 32; ++p) {
         const int qb = (p / 4) % 2;
-        const bf16x2 r = {(__bf16)__builtin_amdgcn_exp2f(fmaf(score(s, p, 0), sl2, -m_run[qb])),
-                          (__bf16)__builtin_amdgcn_exp2f(fmaf(score(s, p, 1), sl2, -m_run[qb]))};
+        const float x0 = __builtin_amdgcn_exp2f(fmaf(score(s, p, 0), sl2, -m_run[qb]));
+        const float x1 = __builtin_amdgcn_exp2f(fmaf(score(s, p, 1), sl2, -m_run[qb]));
+        const bf16x2 r = {(__bf16)x0, (__bf16)x1};
+        if constexpr (LOGS) e_run[qb] += x0 + x1;
         l_run[qb] = __builtin_amdgcn_fdot2_f32_bf16(r, one, l_run[qb], false);
         pf[p / 8][qb][p % 4] = __builtin_bit_cast(uint32_t, r);
       }
@@ -883,6 +890,7 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
     // l_run: the row sum of this lane's row (the fixed-offset pass), or this
     // lane's half of it (the running-max pass)
     const float l_tot = any_fallback ? sum_xor32(l_run[qb]) : l_run[qb];
+    const float e_tot = LOGS ? sum_xor32(e_run[qb]) : 0.f;
     if (!share.cut) {
       const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
       OutRows<D> out(&sV[0][0] + (wave * 2 + qb) * 32 * D);
@@ -893,15 +901,15 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
           out.put(n, 8 * db + 2 * rq + g, acc[qb][db][4 * rq] * inv, acc[qb][db][4 * rq + 1] * inv,
                   acc[qb][db][4 * rq + 2] * inv, acc[qb][db][4 * rq + 3] * inv);
       out.store(a, u, head, wave * 64 + qb * 32, lane);
-      if constexpr (WINDOW) {
+      if constexpr (LOGS) {
         const int row = u.row0 + lrow;
-        if (a.lse && g == 0 && row < u.rows) {
+        if (g == 0 && row < u.rows) {
           const int qi = row / a.group, qh = head * a.group + (row - qi * a.group);
-          a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run[qb], l_tot);
+          a.lse[(int64_t)qh * a.n_tokens + u.q0 + qi] = log_sum(m_run[qb], e_tot);
         }
       }
     } else {
-      float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D);
+      float *pp = a.part + share.slot * seq_part_floats(kSeqRows, D, LOGS);
       float *op = pp + (int64_t)lrow * D;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
@@ -912,6 +920,7 @@ __device__ __forceinline__ void attend128(const SeqArgs &a) {
       if (g == 0) {
         pp[kSeqRows * D + lrow] = l_tot == 0.f ? kMInit : m_run[qb];
         pp[kSeqRows * D + kSeqRows + lrow] = l_tot;
+        if constexpr (LOGS) pp[kSeqRows * D + 2 * kSeqRows + lrow] = e_tot;
       }
     }
   }
@@ -926,6 +935,8 @@ template <bool PAGED>
 __global__ __launch_bounds__(128, 1) void window_attn128_kernel(SeqArgs a) {
   attend128<PAGED ? Keys::kPaged : Keys::kWindow>(a);
 }
+// Packed tensors, with the rows' logarithms.
+__global__ __launch_bounds__(128, 1) void window_logs128_kernel(SeqArgs a) { attend128<Keys::kWindow, true>(a); }
 
 }  // namespace
 
@@ -939,6 +950,7 @@ hipError_t launch_seq128(const SeqArgs &a, hipStream_t s) {
 hipError_t launch_window128(const SeqArgs &a, hipStream_t s) {
   const dim3 grid((uint32_t)seq_groups(a)), block(128);
   if (a.table) hipLaunchKernelGGL((window_attn128_kernel<true>), grid, block, 0, s, a);
+  else if (a.lse) hipLaunchKernelGGL(window_logs128_kernel, grid, block, 0, s, a);
   else hipLaunchKernelGGL((window_attn128_kernel<false>), grid, block, 0, s, a);
   return hipGetLastError();
 }

@@ -430,7 +430,7 @@ hc_status hc_window_workspace(hc_ctx *c, const hc_window_args *p, int64_t *bytes
   SeqArgs a;
   const hc_status st = window_plan(c, p, a);
   if (st != HC_OK) return st;
-  *bytes = part_bytes(a, p->head_dim, kSeqRows);
+  *bytes = part_bytes(a, p->head_dim, kSeqRows, true);       // (with or without lse)
   return HC_OK;
 }
 
@@ -441,7 +441,7 @@ hc_status hc_window_attention(hc_ctx *c, const hc_window_args *p, hc_stream stre
   if (st != HC_OK) return st;
   if (p->n_tokens == 0) return HC_OK;
   if ((st = check_window_tensors(c, p, true)) != HC_OK) return st;
-  if ((st = check_workspace(c, p->workspace, p->workspace_bytes, part_bytes(a, p->head_dim, kSeqRows))) != HC_OK)
+  if ((st = check_workspace(c, p->workspace, p->workspace_bytes, part_bytes(a, p->head_dim, kSeqRows, true))) != HC_OK)
     return st;
   if (a.n_split > 1) use_workspace(a, p->workspace);
   OnDevice on(c->device);

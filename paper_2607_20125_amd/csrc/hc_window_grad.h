@@ -16,10 +16,9 @@ using namespace dev;
 // 5 would do; in return nothing is added up through memory, and the order of every sum is fixed.
 //
 // Roundings.  P and dS are rounded to bf16, the operand type of their products (wider types run at a fraction of its rate); all
-// sums are in 32 bits.  lse is of the rounded probabilities of the forward pass, and rowsum(dO O) of its output as it was
-// rounded, so that dS of a row is off by one small factor and one small offset.  Against 64 bits dQ and dK are off by 0.0024 to
-// 0.0033 of their size (dS alone rounded: 0.0024; in 32 bits throughout, with the result rounded: 0.0017), most where a row sees
-// few keys or weighs few of them.
+// sums are in 32 bits, and so is lse.  rowsum(dO O) is of the forward pass's output as it was rounded, so that dS of a row is off by one
+// small offset.  Against 64 bits dQ and dK are off by 0.0024 to 0.0029 of their size (dS alone rounded: 0.0024; in 32 bits
+// throughout, with the result rounded: 0.0017), most where a row sees few keys or weighs few of them.
 //
 // Both are one scheme.  A wave keeps two stationary operands B1, B2 (32 columns each, in registers as
 // matrix operands) and walks tiles of two streamed tensors A1, A2 (64 rows, in LDS):
