@@ -142,8 +142,9 @@ inline void use_workspace(SeqArgs &a, void *p) {
 }
 
 // --- rotary positions -------------------------------------------------------------------
-// Types, axes and positions of a rotation; fills `a` but for its tensors and turns.
-inline hc_status check_rotation(hc_ctx *c, const hc_rotate_args *p, RotateArgs &a) {
+// Types, axes and positions of a rotation; fills `a` but for its tensors and turns.  none_given: positions of no tokens may
+// be NULL with any axes and grid, as the address of an empty tensor of them is.
+inline hc_status check_rotation(hc_ctx *c, const hc_rotate_args *p, bool none_given, RotateArgs &a) {
   if (p->head_dim < 8 || p->head_dim > kRotMaxDim || p->head_dim % 8 != 0)
     return fail(c, HC_E_INVAL, "head_dim must be a multiple of 8 up to %d", kRotMaxDim);
   for (int type : {p->x_type, p->out_type})
@@ -162,7 +163,7 @@ inline hc_status check_rotation(hc_ctx *c, const hc_rotate_args *p, RotateArgs &
     return fail(c, HC_E_INVAL, "axis_dims must add up to a multiple of 16 up to head_dim");
   if (p->positions) {
     if (!aligned4(p->positions)) return fail(c, HC_E_INVAL, "positions must be 4-byte aligned");
-  } else if (p->n_tokens > 0) {                    // (no positions of no tokens may well be a NULL)
+  } else if (p->n_tokens > 0 || !none_given) {
     if (p->n_axes != 3 || p->grid_h < 1 || p->grid_w < 1)
       return fail(c, HC_E_INVAL, "positions from the grid need three axes, grid_h and grid_w");
     const int64_t frames = p->n_tokens / ((int64_t)p->grid_h * p->grid_w) + 1;

@@ -160,7 +160,7 @@ hc_status hc_rotate(hc_ctx *c, const hc_rotate_args *p, const hc_rotate_tensor *
   if (n_tensors != 1 && n_tensors != 2) return fail(c, HC_E_INVAL, "n_tensors must be 1 or 2");
   if (p->n_tokens < 0) return fail(c, HC_E_INVAL, "n_tokens must not be negative");
   RotateArgs a;
-  hc_status st = check_rotation(c, p, a);
+  hc_status st = check_rotation(c, p, false, a);
   if (st != HC_OK) return st;
   int64_t heads = 0;
   for (int i = 0; i < n_tensors; ++i) {

@@ -18,7 +18,7 @@ hc_status check_norm(hc_ctx *c, const hc_norm_args *p, const void *tensors, int 
     return fail(c, HC_E_INVAL, "weight_type must be HC_BF16 or HC_F32");
   if (!(p->eps >= 0.f) || !std::isfinite(p->eps)) return fail(c, HC_E_INVAL, "eps must be finite and not negative");
   a = NormArgs{};
-  const hc_status st = check_rotation(c, &r, a.rotate);
+  const hc_status st = check_rotation(c, &r, true, a.rotate);
   if (st != HC_OK) return st;
   a.rotate.n_tokens = r.n_tokens;
   a.rotate.head_dim = r.head_dim;
