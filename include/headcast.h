@@ -508,8 +508,9 @@ typedef struct {
 } hc_page_table;
 
 /* Stores rows of k and v as hc_qcache_append does: rows cu_seqlens[s] .. cu_seqlens[s+1] - 1 go to slots
- * start[s], start[s] + 1, ... of sequence s; what has no slot or no page is dropped.  Two rows for the same place of
- * a page: either may remain.  Async. */
+ * start[s], start[s] + 1, ... of sequence s; what has no slot or no page is dropped.  Where several rows of a call have
+ * the same place (tables that name a page twice), each value there is one of theirs, in any mixture; every other place is
+ * as without them.  Async. */
 hc_status hc_paged_append(hc_ctx *ctx, const hc_pages *pages, const hc_page_table *table,
                           const hc_qcache_rows *rows, hc_stream stream);
 

@@ -784,7 +784,8 @@ class Context:
     def paged_append(self, pages: Pages, table, k, v, start, cu_seqlens=None):
         """hc_paged_append: stores the rows of k and v (bf16 [tokens][pages' heads][head_dim]) in slots start[s] ..
         (int32 [n_seqs]) of each sequence; slot i of sequence s is token i % page_tokens of page
-        table[s][i // page_tokens] (int32 [n_seqs][max_pages]).  Rows without a slot or page are dropped."""
+        table[s][i // page_tokens] (int32 [n_seqs][max_pages]).  Rows without a slot or page are dropped; rows for the same place
+        (tables that name a page twice) leave a mixture of their values there."""
         if torch is None:
             _use_torch()
         shape = k.shape
