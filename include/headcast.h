@@ -566,7 +566,8 @@ hc_status hc_window_attention(hc_ctx *ctx, const hc_window_args *args, hc_stream
  * summed over the query heads that share a key head.  p and ds are rounded to bfloat16 for the products, sums are
  * float32, rounded once; repeated calls agree bit for bit.  Token strides of q, k, v and dout are below 2^24, a given
  * softmax_scale not below 2^-100.  Rows outside every sequence are left as they were; a key that
- * no query sees gets zeros.  Async. */
+ * no query sees gets zeros.  A NaN or infinity in a sequence's own rows, seen or not, may reach any of its gradients, and
+ * no other sequence's.  Async. */
 typedef struct {
   hc_window_args forward;
   const void *dout;          /* bf16 [n_tokens][n_heads][head_dim] by the strides below   */

@@ -27,7 +27,7 @@ using namespace dev;
 // With a window, or pages: the key tiles are those of the first tokens and of the window, one behind the other (KeyTiles), and a
 // tile that not every row sees whole is masked key by key, without branches.  Pages are looked up a tile ahead, a run of
 // 16 keys at a time; a run without a page has values of zero and logits of -infinity.  Six prompts of 4000 tokens together
-// (window 512, 4 x 3 heads of 64 dims): 26 us, ten tiles a unit on 1.1 waves a SIMD, 2.4 us each.  (Cut into
+// (window 512, 4 x 3 heads of 64 dims): 26 us, with logarithms 28, ten tiles a unit on 1.1 waves a SIMD, 2.4 us each.  (Cut into
 // ranges for more waves, partial results and their merge cost what it gains: 31 us.)
 //
 // LOGS: the logarithms of the row sums too.  Outputs are divided by the sum of the rounded probabilities, which are what was

@@ -1,5 +1,5 @@
-// Attention over sequences for 128-dim heads on waves of 64 rows: packed keys and values
-// in bf16, or the 4-bit cache.
+// Attention over sequences for 128-dim heads on waves of 64 rows: packed keys and values in bf16, or the 4-bit cache;
+// with a window and first tokens, packed or in pages.
 #include "hc_mask.h"
 #include "hc_window.h"
 
@@ -36,9 +36,10 @@ using namespace dev;
 // With a window, or pages: written-out steps run over the whole tiles among the first tokens, and over those of the window;
 // single steps, masked where they have to be, before, between and behind them.  (One nested loop over both kept more alive
 // than the registers hold: 1.50 ms instead of 1.08.)  Pages: each copy is of a run of 16 rows, whose place comes by a scalar load a tile
-// ahead.  A clip of four 480P blocks, window of two blocks and the first: 1.05 ms, 1.15 PFLOP/s, cores busy 66%; five prompts' 2500 rows
-// over pages of 32, window 4096, 8 x 4 heads: 167-186 us, 0.8-0.9 PFLOP/s, cores busy 47%: masked steps at
-// both ends of a window, and 968 work groups of uneven length on 512 places.
+// ahead.  A clip of four 480P blocks, window of two blocks and the first: 1.03 to 1.12 ms, by the card, 1.08 to 1.17 PFLOP/s, cores busy
+// 66%; five prompts' 2500 rows over pages of 32, window 4096, 8 x 4 heads: 164-194 us, 0.8-0.9 PFLOP/s, cores busy 47%: masked steps at
+// both ends of a window, and 968 work groups of uneven length on 512 places.  With logarithms, 64 additions more a tile: a clip
+// of three blocks, window of one and the first, 635 us, cores busy 60%; without 596, 63%.
 // ---------------------------------------------------------------------------
 constexpr int kPre = 6;      // pairs of the next tile formed during PV
 constexpr int kAhead = 3;    // operand reads in flight

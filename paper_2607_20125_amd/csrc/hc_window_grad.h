@@ -29,7 +29,7 @@ using namespace dev;
 // 8 g .. 8 g + 7 of every 16 (see hc_device.h), in the order that the second products contract.
 //
 // Bound by the matrix cores and the power that they draw with 128-dim heads: forward and gradients of a clip of three 480P blocks (14040
-// tokens, 12 heads, a block sees itself and the first) 2.77 ms, the gradients 2.1-2.2 ms of it, 1.05-1.1 PFLOP/s of the 7 products, cores busy 53%
+// tokens, 12 heads, a block sees itself and the first) 2.75 to 2.9 ms, by the card, the gradients 2.1-2.2 ms of it, 1.05-1.1 PFLOP/s of the 7 products, cores busy 53%
 // at 2.0 GHz.  One wave on a SIMD, so that an operand and all sums stay in its 512 registers; two waves, with half of
 // them, took 7% longer, and left no room for operands that are read 7 products ahead.  Without its copies a step would be 11%
 // faster, without vector instructions 16%, without LDS reads 10% (timed apart).  64-dim heads: two waves on a SIMD; six prompts of
@@ -554,7 +554,7 @@ __device__ __forceinline__ void queries_unit(const GradArgs &a, int block, Share
   const uint16_t *kp = q.k + u.k0 * q.k_token + head * q.k_head, *vp = q.v + u.k0 * q.v_token + head * q.v_head;
   const uint32_t base = lds_addr(&lds.tiles);
   const int n_tiles = __builtin_amdgcn_readfirstlane(tiles.n);
-  // (see grad_keys_kernel; past the last tile the last one again)
+  // (see keys_unit; past the last tile the last one again)
   constexpr int PAIRS = Copier<D>::PAIRS;
   const uint16_t *next_k, *next_v;
   auto prepare = [&](int t) {
@@ -570,7 +570,7 @@ __device__ __forceinline__ void queries_unit(const GradArgs &a, int block, Share
     else copy_v.copy(next_v, to + Streamed<D>::BYTES, part - PAIRS);
   };
   constexpr int COPIES = 2 * Copier<D>::N;
-  // A step as in grad_keys_kernel, with one second product for each operand: dQ.
+  // A step as in keys_unit, with one second product for each operand: dQ.
   struct Scores {
     f32x16 s, t;
   };
